@@ -1,0 +1,104 @@
+/* hh_train.h -- C ABI of what ends a training step on the last pipeline stage: the loss of the output projection with its
+ * gradients, the global gradient norm with clipping, and the optimizer's update.
+ *
+ * The last stage of a pipeline (paper Section 2.3) turns its layers' output into a loss before its backward pass can begin,
+ * and every device ends its step by clipping and applying the gradients that hh_layer_bwd has summed over the micro-batches:
+ *
+ *     hh_layer_fwd ... -> hh_head_step -> hh_layer_bwd ...   (each micro-batch)   -> hh_grad_clip -> hh_adamw_step
+ *
+ * The general rules of hh.h hold: statuses and hh_last_error(), device pointers, buffers that the caller owns, work enqueued on
+ * `stream` without synchronisation, allocation or copies, checks of arguments before any of it.  Every result is the same
+ * from run to run, bit for bit: no sum depends on the order in which workgroups finish.
+ */
+#ifndef HH_TRAIN_H
+#define HH_TRAIN_H
+
+#include "hh.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Output projection and softmax cross entropy.  With z = x W^T [T, V]:
+ *     loss_t = log(sum_v exp z_tv) - z_t,label(t)
+ *     step:  d_tv = g_t (exp(z_tv) / sum_u exp z_tu - [v = label(t)]),  g_t = scale * dloss_t (scale alone where dloss is NULL)
+ *            dx = d W,   dW (+)= d^T x
+ * dx and dW are the gradients of sum_t g_t loss_t; scale is 1 / (tokens that count in the whole batch) for the usual mean.
+ *
+ * A token whose label is negative does not count: its loss is 0, its row of dx is 0 and it adds nothing to dW, whatever its row
+ * of x holds (NaN and infinities too) and whatever its dloss is.  A label of vocab or more is a mistake that only the device
+ * can see: that loss is NaN, and the token adds no gradient.
+ *
+ * The scores z are never kept: the loss alone forms them in registers (HH_BF16) or for a block of tokens at a time; a step
+ * holds them for a block of tokens in the workspace.
+ *
+ * HH_BF16: x, W, dx bfloat16; scores, statistics and losses fp32; dW fp32.  d enters the product for dx as bfloat16 and the one
+ * for dW as a sum of two (16 significant bits), so that dW is an fp32 gradient and not a bfloat16 one in fp32 storage.
+ * HH_F32: everything fp32.
+ *
+ * Shapes: hidden a multiple of 64 (HH_BF16) or 8 (HH_F32), at most 32768; vocab 1 .. 262144, any; tokens >= 1, any; x below 2^31
+ * bytes, W below 2^32 - 2^25 (HH_ERR_UNSUPPORTED_SHAPE otherwise).  The whole vocabulary is on this GPU. */
+typedef struct {
+    int32_t hidden;   /* H */
+    int32_t vocab;    /* V */
+    int32_t tokens;   /* T */
+    int32_t dtype;    /* hh_dtype */
+} hh_head_cfg;
+
+/* Bytes of workspace of hh_head_loss and of hh_head_step (either pointer may be NULL).  Host arithmetic only.  A step's
+ * workspace grows with tokens x vocab up to a block of about 2 GiB of d. */
+int hh_head_sizes(const hh_head_cfg *cfg, size_t *loss_workspace_bytes, size_t *step_workspace_bytes);
+
+/* loss[T] (fp32) of x [T, H] under the weight w [V, H] and labels[T]. */
+int hh_head_loss(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void *w, const int64_t *labels,
+                 float *loss, void *workspace, void *stream);
+
+/* The loss and its gradients.  dloss: [T] fp32 or NULL.  dx [T, H] may be x; dw [V, H] fp32, added to where accumulate != 0. */
+int hh_head_step(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void *w, const int64_t *labels,
+                 const float *dloss, float scale, float *loss, void *dx, float *dw, int accumulate,
+                 void *workspace, void *stream);
+
+/* Global gradient norm and clipping over n tensors of any sizes:
+ *     norm = sqrt(sum of all g^2),  factor = min(1, max_norm / (norm + 1e-6)),  out = factor * g
+ * out == NULL counts a tensor without a clipped copy; out may be g.  Squares are formed and added in fp64, so gradients of any
+ * size can be summed.  A norm that is not finite gives the factor NaN.  Pointers need the alignment of their type
+ * alone (16 bytes for all pointers of a tensor, or the same distance from it, is faster).  tensors is a HOST array, read during the call;
+ * n may be 0, and so may a count, whose pointers are not looked at.
+ * result: device, fp32: result[0] = norm, result[1] = factor. */
+typedef struct {
+    const void *g;    /* gradient, in `dtype` */
+    void *out;        /* clipped copy in the same type, or NULL */
+    int64_t count;    /* elements */
+    int32_t dtype;    /* hh_dtype */
+    int32_t reserved; /* 0 */
+} hh_clip_tensor;
+#define HH_CLIP_WORKSPACE_BYTES ((size_t)8192)
+int hh_grad_clip(hh_ctx *ctx, int n, const hh_clip_tensor *tensors, float max_norm, float *result, void *workspace, void *stream);
+
+/* One step of Adam with decoupled weight decay on n tensors:
+ *     g' = factor * g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
+ *     p = p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + decay p)
+ * in fp32, with constants formed in fp64.  factor: device, fp32, one value (result + 1 of hh_grad_clip: clipped gradients need not be written and read
+ * again), or NULL for 1; a factor that is not finite leaves every tensor as it is.  A bfloat16 parameter has an fp32 master
+ * copy, which is p above, and receives p rounded; an fp32 parameter is its own master copy (master NULL).  step counts from 1.
+ * Pointers, tensors, n and counts as in hh_grad_clip. */
+typedef struct {
+    void *param;
+    float *master;     /* fp32 master copy of a HH_BF16 parameter, NULL for a HH_F32 one */
+    float *m, *v;
+    const void *g;     /* gradient, in grad_dtype */
+    int64_t count;     /* elements */
+    float decay;       /* weight decay of this tensor (0 for norm gains, as a rule) */
+    int32_t param_dtype, grad_dtype;
+    int32_t reserved;  /* 0 */
+} hh_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;      /* >= 1 */
+} hh_adamw_cfg;
+int hh_adamw_step(hh_ctx *ctx, const hh_adamw_cfg *cfg, int n, const hh_adamw_tensor *tensors, const float *factor, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* HH_TRAIN_H */

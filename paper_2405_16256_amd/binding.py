@@ -1,4 +1,4 @@
-"""ctypes binding of libhh.so: the same entry points as include/hh.h, argument marshalling only.
+"""ctypes binding of libhh.so: the same entry points as the headers in include/, argument marshalling only.
 
 Every numeric step runs in the library's HIP kernels.  PyTorch tensors are used
 as owners of device memory (``tensor.data_ptr()``) and for the current stream;
@@ -26,11 +26,13 @@ HH_ERR_DEVICE = -5
 HH_F32 = 0
 HH_BF16 = 1
 HH_STATIC_SCRATCH_BYTES = 128 << 20
+HH_CLIP_WORKSPACE_BYTES = 8192
 
 WEIGHT_FIELDS = ("g_attn", "wq", "wk", "wv", "wo", "g_mlp", "w_gate", "w_up", "w_down")
 EXPORTS = ("hh_last_error", "hh_ctx_create", "hh_ctx_destroy", "hh_ctx_reserve", "hh_layer_flops", "hh_layer_sizes",
            "hh_saved_layout_of", "hh_layer_fwd", "hh_layer_fwd_noalloc", "hh_layer_bwd", "hh_stage_sizes", "hh_stage_step", "hh_stage_step_1f1b", "hh_layer_profile", "hh_trace_begin",
-           "hh_trace_end", "hh_sim_pipeline", "hh_sim_weighted_mean", "hh_plan_layers", "hh_plan_order", "hh_plan_cluster")
+           "hh_trace_end", "hh_sim_pipeline", "hh_sim_weighted_mean", "hh_plan_layers", "hh_plan_order", "hh_plan_cluster",
+           "hh_head_sizes", "hh_head_loss", "hh_head_step", "hh_grad_clip", "hh_adamw_step")
 TRACE_KINDS = ("gemm_nt", "gemm_nn", "gemm_tn", "attn_fwd", "attn_bwd", "elementwise")
 
 
@@ -90,6 +92,23 @@ class hh_cluster_plan(C.Structure):
                 ("grad_allreduce_ms", C.c_double), ("sim", hh_sim_result)]
 
 
+class hh_head_cfg(C.Structure):
+    _fields_ = [("hidden", C.c_int32), ("vocab", C.c_int32), ("tokens", C.c_int32), ("dtype", C.c_int32)]
+
+
+class hh_clip_tensor(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class hh_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("g", C.c_void_p),
+                ("count", C.c_int64), ("decay", C.c_float), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class hh_adamw_cfg(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64)]
+
+
 class HHError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__("hh error %d: %s" % (code, msg))
@@ -131,6 +150,11 @@ def _load() -> C.CDLL:
                           C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(hh_sim_result)],
         "hh_plan_cluster": [C.POINTER(hh_cluster_group), i, C.c_double, i, i, i, i, i, C.c_double, i, C.POINTER(hh_cluster_plan),
                             C.POINTER(C.c_int32), i],
+        "hh_head_sizes": [C.POINTER(hh_head_cfg), sz, sz],
+        "hh_head_loss": [vp, C.POINTER(hh_head_cfg), vp, vp, vp, vp, vp, vp],
+        "hh_head_step": [vp, C.POINTER(hh_head_cfg), vp, vp, vp, vp, C.c_float, vp, vp, vp, i, vp, vp],
+        "hh_grad_clip": [vp, i, C.POINTER(hh_clip_tensor), C.c_float, vp, vp, vp],
+        "hh_adamw_step": [vp, C.POINTER(hh_adamw_cfg), i, C.POINTER(hh_adamw_tensor), vp, vp],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -332,3 +356,83 @@ def hh_plan_cluster(groups: Sequence[hh_cluster_group], cross_link_gbytes_per_s,
     _check(lib.hh_plan_cluster(arr, n, float(cross_link_gbytes_per_s), total_layers, global_batch, micro_batch, seq, hidden,
                                float(flop_per_layer), slack, C.byref(plan), layers, max_stages))
     return plan, list(layers)[:plan.n_stages]
+
+
+# ---------------------------------------------------------------- the end of a training step
+def make_head_cfg(hidden, vocab, tokens, dtype=HH_BF16) -> hh_head_cfg:
+    return hh_head_cfg(hidden, vocab, tokens, dtype)
+
+
+def hh_head_sizes(cfg: hh_head_cfg) -> tuple[int, int]:
+    """-> workspace bytes of (hh_head_loss, hh_head_step)"""
+    a, b = C.c_size_t(), C.c_size_t()
+    _check(lib.hh_head_sizes(C.byref(cfg), C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def hh_head_loss(ctx, cfg: hh_head_cfg, x, w, labels, loss, workspace, stream=0) -> None:
+    """labels: int64, negative where a token does not count."""
+    _check(lib.hh_head_loss(ctx, C.byref(cfg), _ptr(x), _ptr(w), _ptr(labels), _ptr(loss), _ptr(workspace), stream))
+
+
+def hh_head_step(ctx, cfg: hh_head_cfg, x, w, labels, dloss, scale, loss, dx, dw, accumulate, workspace, stream=0) -> None:
+    """dloss: fp32 upstream gradients of the tokens' losses (times scale), or None for scale alone."""
+    _check(lib.hh_head_step(ctx, C.byref(cfg), _ptr(x), _ptr(w), _ptr(labels), _ptr(dloss), float(scale), _ptr(loss), _ptr(dx), _ptr(dw),
+                            int(accumulate), _ptr(workspace), stream))
+
+
+_DTYPES = {torch.float32: HH_F32, torch.bfloat16: HH_BF16}
+
+
+def _dtype(t) -> int:
+    if t.dtype not in _DTYPES:
+        raise TypeError("tensors of a list are float32 or bfloat16, not %s" % t.dtype)
+    return _DTYPES[t.dtype]
+
+
+def _flat(*ts) -> int:
+    """Elements of tensors that go together; they are walked as they lie in memory."""
+    n = ts[0].numel()
+    for t in ts:
+        if not t.is_contiguous() or t.numel() != n:
+            raise ValueError("tensors that go together are contiguous and of one size")
+    return n
+
+
+def make_clip_tensors(pairs: Sequence):
+    """(gradient, tensor for the clipped copy or None) each -> the list that hh_grad_clip takes.  It holds addresses: the tensors
+    have to stay alive as long as it is used."""
+    out = (hh_clip_tensor * len(pairs))()
+    for e, (g, o) in zip(out, pairs):
+        if o is not None and o.dtype != g.dtype:
+            raise TypeError("a clipped copy has its gradient's type")
+        e.g, e.out, e.count, e.dtype = _ptr(g), _ptr(o), _flat(g) if o is None else _flat(g, o), _dtype(g)
+    return out
+
+
+def hh_grad_clip(ctx, tensors, max_norm, result, workspace, stream=0) -> None:
+    """tensors: of make_clip_tensors; result: two fp32 values (norm, factor) on the device; workspace: HH_CLIP_WORKSPACE_BYTES."""
+    _check(lib.hh_grad_clip(ctx, len(tensors), tensors, float(max_norm), _ptr(result), _ptr(workspace), stream))
+
+
+def make_adamw_tensors(rows: Sequence):
+    """(parameter, fp32 master copy or None, m, v, gradient, weight decay) each -> the list that hh_adamw_step takes.  It holds
+    addresses: the tensors have to stay alive as long as it is used."""
+    out = (hh_adamw_tensor * len(rows))()
+    for e, (p, master, m, v, g, decay) in zip(out, rows):
+        for t in (m, v) + (() if master is None else (master,)):
+            if t.dtype != torch.float32:
+                raise TypeError("master copies and moments are float32")
+        e.count = _flat(*(t for t in (p, master, m, v, g) if t is not None))
+        e.param, e.master, e.m, e.v, e.g, e.decay = _ptr(p), _ptr(master), _ptr(m), _ptr(v), _ptr(g), decay
+        e.param_dtype, e.grad_dtype = _dtype(p), _dtype(g)
+    return out
+
+
+def make_adamw_cfg(lr, beta1=0.9, beta2=0.95, eps=1e-8, step=1) -> hh_adamw_cfg:
+    return hh_adamw_cfg(lr, beta1, beta2, eps, step)
+
+
+def hh_adamw_step(ctx, cfg: hh_adamw_cfg, tensors, factor=None, stream=0) -> None:
+    """tensors: of make_adamw_tensors; factor: one fp32 value on the device (result[1:] of hh_grad_clip) or None."""
+    _check(lib.hh_adamw_step(ctx, C.byref(cfg), len(tensors), tensors, _ptr(factor), stream))

@@ -36,6 +36,7 @@
 #include <cstring>
 
 #include "gemm_ring.h"
+#include "gemm_scores.h"
 #include "gemm_tile.h"
 #include "kernels.h"
 
@@ -90,7 +91,8 @@ __device__ __forceinline__ void place_loop() {
 }
 
 // NT or NN; RES: a problem has a residual, which is added to C.  A kernel of its own: what it holds costs the others registers.
-template <int KIND, bool RES>
+// SCORES: the one problem (NT) ends in write_scores: C is z, R the labels, `partial` the statistics, and no tile is cut.
+template <int KIND, bool RES, bool SCORES = false>
 __global__ __launch_bounds__(512) void k_gemm_dma(DmaGroup grp, int full, int n_items, float* __restrict__ partial) {
     // The workgroup walks work items blockIdx.x, + gridDim.x, ... < n_items.  Items below `full` are whole tiles
     // (all of k, written out through the epilogue).  Item full + q is the (q % ksplit)-th share of the k range of
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(512) void k_gemm_dma(DmaGroup grp, int full, int n_
     uint32_t stepA, stepB;
     auto decode = [&](int item) {
         int tix;
-        if (item < full) { tix = item; kbeg = 0; nk = nk_all; slot = -1; }
+        if (SCORES || item < full) { tix = item; kbeg = 0; nk = nk_all; slot = -1; }
         else {
             int tile = slot = item - full;
             const int chunk = split_off(tile, grp.ksplit);
@@ -118,7 +120,7 @@ __global__ __launch_bounds__(512) void k_gemm_dma(DmaGroup grp, int full, int n_
             kbeg = quotient(chunk * nk_all, grp.ksplit);
             nk = quotient((chunk + 1) * nk_all, grp.ksplit) - kbeg;
         }
-        prob = grp.problem_of(tix);
+        prob = SCORES ? 0 : grp.problem_of(tix);
         const DmaProblem& g = grp.p[prob];
         int tm, tn;
         g.map.tile(tix - grp.first[prob], tm, tn);
@@ -242,6 +244,13 @@ __global__ __launch_bounds__(512) void k_gemm_dma(DmaGroup grp, int full, int n_
             fresh = false;
         }
 
+        if constexpr (SCORES) {
+            const DmaProblem& g = grp.p[0];
+            write_scores(acc, cm0 + wm, cn0 + wn, g.M, g.N, (float*)g.C, g.ldc, (const int64_t*)g.R, (float2*)partial,
+                         smem + DSTAGES * 2 * DSTAGE_BYTES + wave * 4096);
+            if (!has_next) return;
+            continue;
+        }
         if (cslot >= 0) {   // a share of the k range: raw fp32 sums, finished by the reduction kernel
             float* pt = partial + (size_t)cslot * (DTILE * DTILE);
 #pragma unroll
@@ -595,13 +604,14 @@ __global__ __launch_bounds__(256) void k_splitk_reduce(const float* __restrict__
     }
 }
 
-// extent in bytes of each operand as laid out in memory (rows x ld), for the buffer bounds
+// extent in bytes of each operand as laid out in memory (rows x ld), for the buffer bounds.  A k-strided A is fetched 8 columns at a
+// time: the last piece of its last row counts as a whole one where the row is that long.
 static long extent_a(const GemmDesc& g) {
-    const long rows = (g.kind == GEMM_TN) ? g.K : g.M, cols = (g.kind == GEMM_TN) ? g.M : g.K;
+    const long rows = (g.kind == GEMM_TN) ? g.K : g.M, cols = (g.kind == GEMM_TN) ? std::min<long>(g.lda, (g.M + 7) & ~7) : g.K;
     return ((rows - 1) * g.lda + cols) * 2;
 }
 static long extent_b(const GemmDesc& g, int K) {
-    const long rows = (g.kind == GEMM_NT) ? g.N : K, cols = (g.kind == GEMM_NT) ? K : g.N;
+    const long rows = g.b_rows ? g.b_rows : (g.kind == GEMM_NT) ? g.N : K, cols = (g.kind == GEMM_NT) ? K : g.N;
     return ((rows - 1) * g.ldb + cols) * 2;
 }
 
@@ -633,16 +643,16 @@ static int tail_shares(const GemmDesc& g, int tiles, int cus) {
 // Full rounds of one tile per compute unit run as one persistent workgroup per unit.  A last, partial round of R
 // tiles would leave most units idle, so it is cut along k into floor(units / R) shares per tile, which the same
 // workgroups take up after their whole tiles (fp32 partials in `ws`, summed in a fixed order by a small second kernel).
-template <int KIND, bool RES>
+template <int KIND, bool RES, bool SCORES>
 static auto dma_kernel() {
     if constexpr (KIND == GEMM_TN) return &k_gemm_dma_tn;
-    else return &k_gemm_dma<KIND, RES>;
+    else return &k_gemm_dma<KIND, RES, SCORES>;
 }
-template <int KIND, bool RES = false>
+template <int KIND, bool RES = false, bool SCORES = false>
 static hipError_t launch_dma(const GemmDesc* g, int n, hipStream_t st) {
     constexpr int LDS = DSTAGES * 2 * DSTAGE_BYTES + 8 * 4096;   // two stages + the epilogue patches of the 8 waves
     static std::atomic<uint64_t> lds_ok{0};
-    auto kern = dma_kernel<KIND, RES>();
+    auto kern = dma_kernel<KIND, RES, SCORES>();
     const hipError_t e = allow_lds((const void*)kern, LDS, lds_ok);
     if (e != hipSuccess) return e;
     hipError_t ce = hipSuccess;
@@ -658,6 +668,13 @@ static hipError_t launch_dma(const GemmDesc* g, int n, hipStream_t st) {
                               q.lda, q.ldb, q.ldc, q.ldr, q.M, q.N, q.accumulate, tile_map(q.M, q.N, DTILE, DTILE)};
         grp.first[i] = tiles;
         tiles += grp.p[i].map.tiles();
+    }
+    if constexpr (SCORES) {
+        grp.p[0].C = g[0].scores->z;
+        grp.p[0].R = (const bf16_t*)g[0].scores->labels;
+        grp.ksplit = divisor(1);
+        kern<<<tiles < NUM_CU ? tiles : NUM_CU, 512, LDS, st>>>(grp, tiles, tiles, (float*)g[0].scores->stats);
+        return hipGetLastError();
     }
     const int ksplit = tail_shares(g[0], tiles, NUM_CU);
     const int tail = ksplit > 1 ? tiles % NUM_CU : 0, full = tiles - tail;
@@ -841,6 +858,12 @@ static double dma_us(long tiles, int nk, double floor, bool ws) {
     return 0.95 * (t + q.t0);   // another kernel has to promise more than the model's bias at these sizes
 }
 
+// w workgroups of ks stages each
+static double rounds_us(const Variant& q, long w, double ks) {
+    const long cap = 256L * q.per_cu, full = w / cap, rem = w % cap;
+    return full * (q.e + ks * q.t_full) + (rem ? q.e + ks * (rem <= 256 ? stage_us(q, rem, ks) : q.t_full) : 0.0);
+}
+
 // One problem.  whole_only: it has to run as one piece (B in several segments), which the 256x256 kernel cannot.
 static Plan plan_one(const GemmDesc& g, bool whole_only) {
     const int nk = (g.K + DK - 1) / DK;
@@ -850,7 +873,6 @@ static Plan plan_one(const GemmDesc& g, bool whole_only) {
         const Variant& q = VARIANTS[v];
         const long tiles = tiles_of(g, q);
         if ((v == V_DMA && (whole_only || tiles < 64)) || (q.nt_only && g.kind != GEMM_NT)) continue;
-        const long cap = 256L * q.per_cu;
         if (v == V_DMA) {
             const double t = dma_us(tiles, nk, floor, g.ws != nullptr);
             if (t < best.t) best = Plan{V_DMA, {1}, {0}, t};
@@ -858,10 +880,7 @@ static Plan plan_one(const GemmDesc& g, bool whole_only) {
         }
         for (const int s : SPLITS) {
             if (!may_split(g, q, s)) break;
-            const long w = tiles * s, full = w / cap, rem = w % cap;
-            const double ks = (double)nk / s;
-            double t = full * (q.e + ks * q.t_full) + (rem ? q.e + ks * (rem <= 256 ? stage_us(q, rem, ks) : q.t_full) : 0.0);
-            if (t < floor) t = floor;
+            double t = std::max(rounds_us(q, tiles * s, (double)nk / s), floor);
             if (s > 1) t += 3.0 + reduce_us(g, q, s);
             t += q.t0;
             if (t < best.t) best = Plan{v, {s}, {0}, t};
@@ -1040,8 +1059,15 @@ static int segments(const GemmDesc& g, GemmDesc out[3]) {
 
 static hipError_t check(const GemmDesc& g) {
     const long a_bytes = extent_a(g), b_bytes = extent_b(g, g.K);
+    // 32-bit byte offsets, which run past the end by at most the 256 rows of a tile
     if (a_bytes >= (1L << 32) - (1L << 25) || b_bytes >= (1L << 32) - (1L << 25)) return hipErrorInvalidValue;
-    if (g.lda > 65535 || g.ldb > 65535) return hipErrorInvalidValue;
+    if (g.lda > MAX_LD || g.ldb > MAX_LD || a_bytes + 512L * g.lda >= (1L << 32) || b_bytes + 512L * g.ldb >= (1L << 32)) return hipErrorInvalidValue;
+    if (g.b_rows && (g.k1 || g.b_rows < 0 || g.b_rows > (g.kind == GEMM_NT ? g.N : g.K))) return hipErrorInvalidValue;
+    if (g.scores) {
+        const GemmScores& s = *g.scores;
+        if (g.kind != GEMM_NT || g.K % 64 || g.R || g.fuse.kind || g.norm || g.micro > 1 || !s.stats || !s.labels) return hipErrorInvalidValue;
+        return s.z && (g.ldc < ((g.N + 3) & ~3) || (long)g.M * g.ldc * 4 >= (1L << 31)) ? hipErrorInvalidValue : hipSuccess;
+    }
     // C (and the residual) are addressed with 32-bit byte offsets below 2 GB
     if (((long)(g.M - 1) * g.ldc + g.N) * (g.out_f32 ? 4 : 2) >= (1L << 31)) return hipErrorInvalidValue;
     if (g.R && ((long)(g.M - 1) * g.ldr + g.N) * 2 >= (1L << 31)) return hipErrorInvalidValue;
@@ -1197,6 +1223,41 @@ static hipError_t micro_launches(const GemmDesc* g, int n, const Route& r, L lau
     return e;
 }
 
+// Scores: the variants whose waves own 64 columns, uncut.
+template <int BM, int BN, int WM, int WN, int NS>
+static hipError_t launch_ring_scores(const GemmDesc& g, hipStream_t st) {
+    constexpr int LDS = NS * (BM + BN) * DK * 2;
+    static std::atomic<uint64_t> lds_ok{0};
+    auto kern = &k_gemm_ring_scores<BM, BN, WM, WN, NS>;
+    const hipError_t e = allow_lds((const void*)kern, LDS, lds_ok);
+    if (e != hipSuccess) return e;
+    RingProblem<1, false> p{};
+    p.A.p[0] = const_cast<void*>(g.A); p.B.p[0] = const_cast<void*>(g.B); p.C.p[0] = g.scores->z;
+    p.R.p[0] = const_cast<int64_t*>(g.scores->labels);
+    p.partial = (float*)g.scores->stats;
+    p.kseg[0] = p.kseg[1] = INT_MAX;
+    p.a_bytes = (uint32_t)extent_a(g); p.b_bytes = (uint32_t)extent_b(g, g.K);
+    p.lda = g.lda; p.ldb = g.ldb; p.ldc = g.ldc; p.M = g.M; p.N = g.N; p.K = g.K;
+    p.micro = p.seq = 1; p.nk = g.K / DK;
+    p.map = tile_map(g.M, g.N, BM, BN);
+    const int tiles = p.map.tiles();
+    p.tiles = p.items = divisor(tiles); p.ksplit = divisor(1);
+    kern<<<tiles, WM * WN * 64, LDS, st>>>(p);
+    return hipGetLastError();
+}
+static hipError_t gemm_scores(const GemmDesc& g, hipStream_t st) {
+    const int nk = g.K / DK;
+    int best = V_DMA;
+    double t = tiles_of(g, VARIANTS[V_DMA]) < 64 ? 1e30 : dma_us(tiles_of(g, VARIANTS[V_DMA]), nk, 0.0, false);
+    for (const int v : {V_64x128, V_128x256}) {
+        const double u = rounds_us(VARIANTS[v], tiles_of(g, VARIANTS[v]), nk) + VARIANTS[v].t0;
+        if (u < t) { t = u; best = v; }
+    }
+    if (best == V_64x128) return launch_ring_scores<64, 128, 2, 2, 3>(g, st);
+    if (best == V_128x256) return launch_ring_scores<128, 256, 2, 4, 3>(g, st);
+    return launch_dma<GEMM_NT, false, true>(&g, 1, st);
+}
+
 hipError_t gemm_bf16(const GemmDesc* g, int n, hipStream_t st) {
     if (n < 1 || n > DMA_MAX) return hipErrorInvalidValue;
     for (int i = 0; i < n; i++) {
@@ -1205,6 +1266,7 @@ hipError_t gemm_bf16(const GemmDesc* g, int n, hipStream_t st) {
         if (e != hipSuccess) return e;
         if ((g[i].kind == GEMM_NT) != (g[0].kind == GEMM_NT)) return hipErrorInvalidValue;
     }
+    if (g[0].scores) return n == 1 ? gemm_scores(g[0], st) : hipErrorInvalidValue;
     Route r;
     route(g, n, r);
     for (int i = 0; i < n; i++)   // several micro-batches, fusions: where gemm_bf16_on_ring says so

@@ -318,12 +318,13 @@ static hipError_t gemm_f32_f(const GemmDesc* d, int n, hipStream_t st) {
     for (int i = 0; i < n; i++) {
         const GemmDesc& g = d[i];
         if (g.M <= 0 || g.N <= 0 || g.K <= 0 || g.k1 || (g.kind == GEMM_NT) != (d[0].kind == GEMM_NT)) return hipErrorInvalidValue;
-        const long a_rows = (g.kind == GEMM_TN) ? g.K : g.M, a_cols = (g.kind == GEMM_TN) ? g.M : g.K;
-        const long b_rows = (g.kind == GEMM_NT) ? g.N : g.K, b_cols = (g.kind == GEMM_NT) ? g.K : g.N;
+        const long a_rows = (g.kind == GEMM_TN) ? g.K : g.M, a_cols = (g.kind == GEMM_TN) ? std::min<long>(g.lda, (g.M + 3) & ~3) : g.K;
+        const long b_rows = g.b_rows ? g.b_rows : (g.kind == GEMM_NT) ? g.N : g.K, b_cols = (g.kind == GEMM_NT) ? g.K : g.N;
         const long a_bytes = ((a_rows - 1) * g.lda + a_cols) * 4, b_bytes = ((b_rows - 1) * g.ldb + b_cols) * 4;
         // 32-bit byte offsets with room for a tile of rows, past the end
         if (a_bytes >= (1L << 32) - (1L << 25) || b_bytes >= (1L << 32) - (1L << 25)) return hipErrorInvalidValue;
-        if (g.lda > 65535 || g.ldb > 65535 || g.N % 4 != 0) return hipErrorInvalidValue;
+        if (g.lda > MAX_LD || g.ldb > MAX_LD || a_bytes + 256L * g.lda >= (1L << 32) || b_bytes + 256L * g.ldb >= (1L << 32) || g.N % 4 != 0) return hipErrorInvalidValue;
+        if (g.scores || (g.b_rows && (g.k1 || g.b_rows < 0 || g.b_rows > (g.kind == GEMM_NT ? g.N : g.K)))) return hipErrorInvalidValue;
         if (g.kind != GEMM_TN && g.K % 4 != 0) return hipErrorInvalidValue;
         F32Problem<F, MB>& p = grp.p[i];
         if (g.micro < 1 || g.micro > MB || g.micro != d[0].micro || (MB > 1 && !g.each)) return hipErrorInvalidValue;

@@ -8,6 +8,7 @@
 #pragma once
 #include <type_traits>
 
+#include "gemm_scores.h"
 #include "gemm_tile.h"
 #include "kernels.h"
 
@@ -80,7 +81,8 @@ __device__ __forceinline__ float rotated(float v) { return __int_as_float(__buil
 // LDS for all of k; only B goes through the ring.  Bound by latency: the launch before it (3.6 us with the gap behind it, of rows of 256)
 // goes, and the workgroups get 1.2 to 1.9 us longer, for about 500 instructions between x and its place in LDS and because what waits for
 // x and the gain, which the compiler counts, waits for the requests of B behind them too.
-template <int KIND, int MB, bool F, int BM, int BN, int WM, int WN, int NS, bool NORM = false>
+// SCORES: the tile ends in write_scores: C is z, R the labels, `partial` the statistics.
+template <int KIND, int MB, bool F, int BM, int BN, int WM, int WN, int NS, bool NORM = false, bool SCORES = false>
 __device__ __forceinline__ void ring_body(const RingProblem<MB, F>& g, const RingNorm<MB>* norm = nullptr, bool writer = false) {
     if constexpr (NORM) asm volatile("" ::"s"(norm->gain), "s"(norm->eps), "s"(g.K), "s"(g.M), "s"(g.N));
     // what the first operand requests need, loaded at once
@@ -325,7 +327,7 @@ __device__ __forceinline__ void ring_body(const RingProblem<MB, F>& g, const Rin
     // Of three or four blocks a wave, 64 registers, it costs more than it gives (1100x3072x3072 with residual 27.4 -> 28.2), and
     // gate|up, two tiles as large as the product, hold up the k tiles behind them (700x2048x1024 12.2 -> 12.6).  The wait for k tile 0
     // leaves as many requests on their way as the later tiles have, so it covers as many of those as are asked for here.
-    constexpr bool EARLY = TM * TN <= 2 && !(KIND == GEMM_NN && FUSES);
+    constexpr bool EARLY = TM * TN <= 2 && !(KIND == GEMM_NN && FUSES) && !SCORES;
     Beside beside[EARLY ? TM : 1][EARLY ? TN : 1];
     if (EARLY && ksplit == 1 && !SUMS) {
 #pragma unroll
@@ -508,6 +510,12 @@ __device__ __forceinline__ void ring_body(const RingProblem<MB, F>& g, const Rin
         }
     }
 
+    if constexpr (SCORES) {
+        __syncthreads();   // nobody reads the ring any more
+        write_scores(acc, m0 + wm, n0 + wn, M, N, (float*)Cv, ldc, (const int64_t*)R, (float2*)g.partial, smem + wave * 4096);
+        return;
+    }
+
     // a share of the k range, or one micro-batch's product of several: raw fp32 sums, finished by k_ring_reduce
     if (ksplit > 1 || (SUMS && seq == 1)) {
         float* pt = g.partial + (((size_t)(tm * tiles_n + tn) * (MB == 1 ? 1 : g.micro) + micro) * ksplit + share) * (BM * BN);
@@ -626,6 +634,12 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN / (WM * WN) > 64 * 128 ? 1 : 
     if (!BWD) ring_body<GEMM_NT, MB, F, BM, BN, WM, WN, NS>(g);
     else if (F || !(tn >> i & 1)) ring_body<GEMM_NN, MB, F, BM, BN, WM, WN, NS>(g);
     else ring_body<GEMM_TN, MB, F, BM, BN, WM, WN, NS>(g);
+}
+
+// one problem whose result is scores
+template <int BM, int BN, int WM, int WN, int NS>
+__global__ __launch_bounds__(WM * WN * 64, BM * BN / (WM * WN) > 64 * 128 ? 1 : 2) void k_gemm_ring_scores(RingProblem<1, false> g) {
+    ring_body<GEMM_NT, 1, false, BM, BN, WM, WN, NS, false, true>(g);
 }
 
 // NT problems that norm the rows of A, which they share

@@ -1,0 +1,148 @@
+// Softmax cross entropy over a vocabulary: what comes between the product that forms the scores and the two that take their
+// gradient.
+//
+// Row t of z has the statistics (largest score, sum of exponentials) of each slot of its columns.  k_head_rows puts them together,
+//     m = max_s m_s,  lse = m + log(sum_s S_s exp(m_s - m)),
+// and k_head_grad reads the scores once and writes d_tv = g_t (exp(z_tv - lse_t) - [v = label(t)]).  All of it in fp32.
+#include "common.h"
+#include "kernels.h"
+
+namespace hh {
+
+constexpr float LOG2_E = 1.4426950408889634f;
+
+// (m, s) and (m1, s1) as one; -inf with 0 is nothing
+__device__ __forceinline__ void join(float& m, float& s, float m1, float s1) {
+    const float top = fmaxf(m, m1), ref = top == -INFINITY ? 0.f : top;
+    s = s * __builtin_amdgcn_exp2f((m - ref) * LOG2_E) + s1 * __builtin_amdgcn_exp2f((m1 - ref) * LOG2_E);
+    m = top;
+}
+
+// ------------------------------------------------------------------ statistics of fp32 scores
+// A workgroup reads HEAD_F32_SLOT columns of one row.  (In bf16 the product's own epilogue forms them.)
+__global__ __launch_bounds__(256) void k_head_stats(const float* __restrict__ z, int ldz, const int64_t* __restrict__ labels,
+                                                    float2* __restrict__ stats, int M, int N) {
+    const int row = (int)blockIdx.y, slot = (int)blockIdx.x, col = slot * HEAD_F32_SLOT + 4 * (int)threadIdx.x;
+    float f[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (col < N) {
+        Vec<float>::load(z + (size_t)row * ldz + col, f);   // rows are padded
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (col + e >= N) f[e] = -INFINITY;
+    }
+    const int64_t label = labels[row];
+    if (label >= col && label < col + 4 && label < N)
+        ((float*)(stats + (size_t)gridDim.x * M))[row] = label == col ? f[0] : label == col + 1 ? f[1] : label == col + 2 ? f[2] : f[3];
+    __shared__ float red[8];
+    float top = wave_max(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; e++) sum += __builtin_amdgcn_exp2f((f[e] - ref) * LOG2_E);
+    sum = block_sum<4>(sum, red + 4);
+    if (threadIdx.x == 0) stats[(size_t)slot * M + row] = make_float2(top, sum);
+}
+
+hipError_t head_stats_f32(const float* z, int ldz, const int64_t* labels, float2* stats, int M, int N, hipStream_t st) {
+    k_head_stats<<<dim3((N + HEAD_F32_SLOT - 1) / HEAD_F32_SLOT, M), 256, 0, st>>>(z, ldz, labels, stats, M, N);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ rows
+// 16 rows a workgroup, 64 threads a row: 16 neighbouring rows of a slot are 128 bytes.
+constexpr int ROWS_WG = 16;
+__global__ __launch_bounds__(1024) void k_head_rows(const float2* __restrict__ stats, int slots, const int64_t* __restrict__ labels, int M, int N,
+                                                    const float* __restrict__ dloss, float scale, float* __restrict__ loss, float2* __restrict__ rows) {
+    __shared__ float2 part[16][ROWS_WG];
+    const int r = threadIdx.x & 15, row = (int)blockIdx.x * ROWS_WG + r, from = threadIdx.x >> 4;
+    float m = -INFINITY, s = 0.f;
+    if (row < M)
+        for (int i = from; i < slots; i += 64) {
+            const float2 v = stats[(size_t)i * M + row];
+            join(m, s, v.x, v.y);
+        }
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+        const float m1 = __shfl_xor(m, o, WAVE), s1 = __shfl_xor(s, o, WAVE);
+        join(m, s, m1, s1);
+    }
+    if ((threadIdx.x & 63) < ROWS_WG) part[threadIdx.x >> 6][r] = make_float2(m, s);
+    __syncthreads();
+    if (threadIdx.x >= ROWS_WG || row >= M) return;
+    m = part[0][r].x; s = part[0][r].y;
+    for (int w = 1; w < 16; w++) join(m, s, part[w][r].x, part[w][r].y);
+    const float lse = m + logf(s);
+    const int64_t label = labels[row];
+    const bool counts = label >= 0 && label < N;
+    const float* const picked = (const float*)(stats + (size_t)slots * M);
+    loss[row] = counts ? lse - picked[row] : label < 0 ? 0.f : __builtin_nanf("");
+    // the column of the one-hot vector, -1 where the token does not count, beside what k_head_grad multiplies by
+    if (rows) rows[row] = make_float2(lse, counts ? (dloss ? scale * dloss[row] : scale) : 0.f);
+}
+
+hipError_t head_rows(const float2* stats, int slots, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
+                     float2* rows, hipStream_t st) {
+    k_head_rows<<<(M + ROWS_WG - 1) / ROWS_WG, 1024, 0, st>>>(stats, slots, labels, M, N, dloss, scale, loss, rows);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ gradient of the scores
+// A workgroup turns 1024 scores of a row into d; columns N .. ldz-1 become zeros, and so do rows that do not count, whatever their
+// scores are.  bf16: d is written as hi + lo, two bf16 numbers, lo `lo_rows` rows behind hi.  The workgroups past those of
+// the scores copy the row's x, zeros where the token does not count (zero times NaN would be NaN in dW), for bf16
+// beside lo as well: d^T x is then one product over hi's rows and lo's.
+template <typename T>
+__global__ __launch_bounds__(256) void k_head_grad(const float* z, int ldz, const float2* __restrict__ rows, const int64_t* __restrict__ labels,
+                                                   int N, T* d, int lo_rows, const T* __restrict__ x, T* __restrict__ xs, int H, int z_wgs) {
+    constexpr bool TWO = sizeof(T) == 2;
+    constexpr int PER = 1024;
+    const int row = (int)blockIdx.y;
+    const int64_t label = labels[row];
+    const bool counts = label >= 0 && label < N;
+    if ((int)blockIdx.x >= z_wgs) {
+        constexpr int VN = Vec<T>::N;
+        const int col = ((int)blockIdx.x - z_wgs) * (256 * VN) + VN * (int)threadIdx.x;
+        if (col >= H) return;
+        typename Vec<T>::Raw v{};
+        if (counts) v = Vec<T>::raw(x + (size_t)row * H + col);
+        *reinterpret_cast<typename Vec<T>::Raw*>(xs + (size_t)row * H + col) = v;
+        if (TWO) *reinterpret_cast<typename Vec<T>::Raw*>(xs + (size_t)(row + lo_rows) * H + col) = v;
+        return;
+    }
+    const int col = (int)blockIdx.x * PER + 4 * (int)threadIdx.x;
+    if (col >= ldz) return;
+    float f[4] = {0.f, 0.f, 0.f, 0.f};
+    if (counts && col < N) {
+        const float2 r = rows[row];
+        Vec<float>::load(z + (size_t)row * ldz + col, f);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const float p = __builtin_amdgcn_exp2f((f[e] - r.x) * LOG2_E);
+            f[e] = col + e < N ? r.y * (label == col + e ? p - 1.f : p) : 0.f;
+        }
+    }
+    const size_t at = (size_t)row * ldz + col;
+    if constexpr (TWO) {
+        const uint2 hi = make_uint2(pack_bf2(f[0], f[1]), pack_bf2(f[2], f[3]));
+        const uint2 lo = make_uint2(pack_bf2(f[0] - lo_bf(hi.x), f[1] - hi_bf(hi.x)), pack_bf2(f[2] - lo_bf(hi.y), f[3] - hi_bf(hi.y)));
+        *reinterpret_cast<uint2*>(d + at) = hi;
+        *reinterpret_cast<uint2*>(d + at + (size_t)lo_rows * ldz) = lo;
+    } else {
+        Vec<float>::store((float*)d + at, f);   // in place of the scores
+    }
+}
+
+hipError_t head_grad(int dtype, const float* z, int ldz, const float2* rows, const int64_t* labels, int M, int N, void* d, int lo_rows,
+                     const void* x, void* xs, int H, hipStream_t st) {
+    const int z_wgs = (ldz + 1023) / 1024;
+    if (dtype == DT_BF16)
+        k_head_grad<bf16_t><<<dim3(z_wgs + (H + 2047) / 2048, M), 256, 0, st>>>(z, ldz, rows, labels, N, (bf16_t*)d, lo_rows, (const bf16_t*)x, (bf16_t*)xs, H, z_wgs);
+    else
+        k_head_grad<float><<<dim3(z_wgs + (H + 1023) / 1024, M), 256, 0, st>>>(z, ldz, rows, labels, N, (float*)d, lo_rows, (const float*)x, (float*)xs, H, z_wgs);
+    return hipGetLastError();
+}
+
+}  // namespace hh

@@ -1,8 +1,6 @@
 // C ABI of the decoder-stage library: argument validation, buffer carving and
 // the order in which the gfx950 kernels are enqueued.  No numeric work happens
 // on the host except the rotary cos/sin table (built once per context).
-#include "../../include/hh.h"
-
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -14,6 +12,7 @@
 #include <new>
 #include <vector>
 
+#include "ctx.h"
 #include "kernels.h"
 
 namespace hh {
@@ -86,51 +85,23 @@ static_assert(HH_STATIC_SCRATCH_BYTES == STATIC_SCRATCH_BYTES, "the header state
 // ------------------------------------------------------------------ errors
 static thread_local char g_err[512] = "";
 
-static int fail(int code, const char* fmt, ...) {
+namespace hh {
+int fail(int code, const char* fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_err, sizeof g_err, fmt, ap);
     va_end(ap);
     return code;
 }
-static int hip_fail(hipError_t e, const char* what) {
+int hip_fail(hipError_t e, const char* what) {
     return fail(HH_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
-#define HIP_TRY(call)                                        \
-    do {                                                     \
-        hipError_t e_ = (call);                              \
-        if (e_ != hipSuccess) return hip_fail(e_, #call);    \
-    } while (0)
-
-extern "C" const char* hh_last_error(void) { return g_err; }
-namespace hh {
 // for the other translation units of the library
 int set_error(int code, const char* msg) { return fail(code, "%s", msg); }
 }  // namespace hh
 
+extern "C" const char* hh_last_error(void) { return g_err; }
 // ------------------------------------------------------------------ context
-struct TraceRec {
-    hipEvent_t a, b;
-    int kind;
-    double work;
-    size_t events;  // the record whose events bracket the launch (its own, unless GEMMs share one)
-    double share;   // of the time between them that is this family's
-    int count;      // micro-batches that the launch takes side by side: it stands for a launch of each
-};
-struct hh_ctx {
-    int device;
-    float* rope_table;  // device: cos[S][d/2] then sin[S][d/2]
-    int rope_seq, rope_dim;
-    float rope_base;
-    std::vector<TraceRec> trace;  // events created by hh_trace_begin
-    size_t trace_used;
-    bool trace_on;
-    uint32_t trace_mask;          // families recorded while trace_on
-    void* gemm_ws;                // k-split scratch inside the caller's workspace, set by each hot call
-    size_t gemm_room;             // its bytes where several micro-batches go side by side, set by each such call
-    std::vector<float*> retired_tables;   // rotary tables replaced by a larger one: freed with the context
-};
-
 extern "C" int hh_ctx_create(hh_ctx** out, int device) {
     if (!out) return fail(HH_ERR_INVALID_ARG, "hh_ctx_create: out is NULL");
     *out = nullptr;
@@ -194,17 +165,11 @@ static int check_cfg(const hh_layer_cfg* c) {
     return HH_OK;
 }
 
-static int check_ptr(const void* p, const char* name) {
+int hh::check_ptr(const void* p, const char* name) {
     if (!p) return fail(HH_ERR_INVALID_ARG, "%s is NULL", name);
     if ((uintptr_t)p & 15) return fail(HH_ERR_MISALIGNED, "%s is not 16-byte aligned", name);
     return HH_OK;
 }
-#define TRY(x)                \
-    do {                      \
-        int rc_ = (x);        \
-        if (rc_ != HH_OK) return rc_; \
-    } while (0)
-
 static int check_weights(const hh_layer_weights* w) {
     if (!w) return fail(HH_ERR_INVALID_ARG, "weights is NULL");
     TRY(check_ptr(w->g_attn, "weights.g_attn")); TRY(check_ptr(w->wq, "weights.wq")); TRY(check_ptr(w->wk, "weights.wk"));
@@ -221,7 +186,6 @@ static int check_grads(const hh_layer_grads* g) {
 }
 
 // ------------------------------------------------------------ buffer layouts
-static inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Dims {
     int T, H, A, Akv, Q3, F, S, B, nh, nkv, d, dt;   // Akv = nkv*d; Q3 = A + 2*Akv: width of a q|k|v row
@@ -375,19 +339,6 @@ extern "C" int hh_ctx_reserve(hh_ctx* ctx, const hh_layer_cfg* cfg) {
 }
 
 // ------------------------------------------------------------------ tracing
-// When tracing is on, every kernel-family launch is bracketed by two events on the
-// launch stream; hh_trace_end turns them into per-family time and work sums.
-struct Traced {
-    hh_ctx* ctx; hipStream_t st; TraceRec* rec;
-    Traced(hh_ctx* c, hipStream_t s, int kind, int count, double work) : ctx(c), st(s), rec(nullptr) {
-        if (c->trace_on && ((c->trace_mask >> kind) & 1u) && c->trace_used < c->trace.size()) {
-            rec = &c->trace[c->trace_used++];
-            rec->kind = kind; rec->work = work * count; rec->events = ctx->trace_used - 1; rec->share = 1.0; rec->count = count;
-            (void)hipEventRecord(rec->a, st);
-        }
-    }
-    ~Traced() { if (rec) (void)hipEventRecord(rec->b, st); }
-};
 #define TR(kind, work, call)                     \
     do {                                         \
         Traced t_(ctx, st, (kind), p.n, (double)(work)); \
@@ -398,7 +349,7 @@ static double gemm_flop(const GemmDesc& g) { return 2.0 * g.M * g.N * g.K * g.mi
 static void gemm_scratch(const hh_ctx* ctx, GemmDesc& g) { g.ws = ctx->gemm_ws; g.ws_bytes = ctx->gemm_ws ? GEMM_WS_BYTES : 0; g.ws_room = ctx->gemm_room; }
 // A group of GEMMs in one call.  Where they share a launch it is bracketed once and its time shared out to the members by
 // their flops; members with launches of their own are traced (and launched, in the same way) one by one.
-static hipError_t tgemm(hh_ctx* ctx, int dt, GemmDesc* g, int n, hipStream_t st) {
+hipError_t hh::tgemm(hh_ctx* ctx, int dt, GemmDesc* g, int n, hipStream_t st) {
     double total = 0.0;
     for (int i = 0; i < n; i++) {
         gemm_scratch(ctx, g[i]);
@@ -421,7 +372,6 @@ static hipError_t tgemm(hh_ctx* ctx, int dt, GemmDesc* g, int n, hipStream_t st)
     if (traced) (void)hipEventRecord(ctx->trace[first].b, st);
     return e;
 }
-static hipError_t tgemm(hh_ctx* ctx, int dt, GemmDesc g, hipStream_t st) { return tgemm(ctx, dt, &g, 1, st); }
 
 extern "C" int hh_trace_begin(hh_ctx* ctx, int max_launches, uint32_t kind_mask) {
     if (!ctx) return fail(HH_ERR_INVALID_ARG, "ctx is NULL");
@@ -458,17 +408,15 @@ extern "C" int hh_trace_end(hh_ctx* ctx, hh_trace_sum* out, int n_kinds) {
 }
 
 // ------------------------------------------------------------ layer forward
-static inline char* at(void* base, size_t off) { return (char*)base + off; }
-static inline const char* at(const void* base, size_t off) { return (const char*)base + off; }
 
-static GemmDesc desc(int kind, int M, int N, int K, const void* A, int lda, const void* B, int ldb, void* C, int ldc,
-                     const void* R = nullptr, int ldr = 0, int out_f32 = 0, int acc = 0) {
+GemmDesc hh::desc(int kind, int M, int N, int K, const void* A, int lda, const void* B, int ldb, void* C, int ldc,
+                  const void* R, int ldr, int out_f32, int acc) {
     GemmDesc g;
     g.kind = kind; g.M = M; g.N = N; g.K = K; g.A = A; g.lda = lda; g.B = B; g.ldb = ldb; g.C = C; g.ldc = ldc;
     g.R = R; g.ldr = ldr; g.out_f32 = out_f32; g.accumulate = acc; g.ws = nullptr; g.ws_bytes = 0;
     g.B1 = g.B2 = nullptr; g.k1 = g.k2 = 0;
-    g.fuse = GemmFuse{}; g.split = nullptr; g.norm = nullptr;
-    g.micro = 1; g.each = nullptr;
+    g.fuse = GemmFuse{}; g.split = nullptr; g.norm = nullptr; g.scores = nullptr;
+    g.b_rows = 0; g.micro = 1; g.each = nullptr;
     return g;
 }
 

@@ -44,11 +44,17 @@ constexpr int SPLIT_ROW = 16384, SPLIT_COLUMNS = SPLIT_ROW / 2;
 // The RMSNorm of the rows of A on the way into an NT launch: xn and r (of each micro-batch) are written beside the product.
 struct GemmNorm { Each xn, r; const void* gain; float eps; };
 constexpr int NORM_K = 256;
+// An NT launch (bf16) whose result is scores [M, N] over a vocabulary of any size N: fp32 in z (rows of ldc; null: not written),
+// the largest score of a row and the sum of exp(score - largest) for each SCORE_SLOT columns in stats [slot][M], and behind
+// those, [M] floats, the score of the row's label (of a label that is no column: nothing).
+constexpr int SCORE_SLOT = 64;
+struct GemmScores { float* z; float2* stats; const int64_t* labels; };
 struct GemmDesc {
     int kind;
     int M, N, K;
     const void* A; int lda;
     const void* B; int ldb;
+    int b_rows;              // rows of B that are there (0: as many as the product has); the others read as zeros
     void* C; int ldc;
     const void* R; int ldr;  // optional residual in the storage dtype, added before rounding (NULL: none)
     int out_f32;             // 1: C is fp32 regardless of the storage dtype (parameter gradients)
@@ -62,9 +68,11 @@ struct GemmDesc {
     GemmFuse fuse;
     GemmSplit* split;        // not null: the launch may leave its partial sums (ksplit > 1 then, else C is complete)
     const GemmNorm* norm;    // not null (bf16, where gemm_bf16_norms): A holds x, and xn takes its place; one for a launch
+    const GemmScores* scores;   // not null (NT, bf16): C stays unused
     int micro;               // micro-batches; above 1 (bf16: where gemm_bf16_on_ring) their operands are in `each`
     const GemmMicro* each;
 };
+constexpr int MAX_LD = 1 << 18;   // elements of an operand's row, a vocabulary among them
 constexpr size_t GEMM_WS_BYTES = (size_t)64 << 20;   // enough for 256 partial tiles of 256x256 fp32
 
 // The library's own scratch array (one per GPU, held until the process ends) and its size.
@@ -131,5 +139,38 @@ size_t attn_bwd_scratch_bytes(int dtype, int B, int S, int nh, int nkv, int d);
 hipError_t attn_bwd(int dtype, const void* qkv, int ld, const void* o, const void* dout, const float* lse,
                     float* dvec, void* dqkv, void* scratch, size_t scratch_bytes, int B, int S, int nh, int nkv, int d,
                     const float* rope_table, int rope_seq, const MicroStride& micro, hipStream_t st);
+
+// ---- output projection and softmax cross entropy (head.hip).  stats: [slot][M] (largest score, sum of exponentials) and behind them
+// [M] floats, the labels' scores, as of GemmScores.
+// The same of fp32 scores [M, N] in rows of ldz, slots of HEAD_F32_SLOT columns.
+constexpr int HEAD_F32_SLOT = 1024;
+hipError_t head_stats_f32(const float* z, int ldz, const int64_t* labels, float2* stats, int M, int N, hipStream_t st);
+// loss[M], and in rows[M] (null: none) the log-sum-exp of a row and the upstream gradient of its loss, 0 where it does not count
+hipError_t head_rows(const float2* stats, int slots, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
+                     float2* rows, hipStream_t st);
+// d from the scores z (rows of ldz both, the padding zeros), in bf16 as two matrices, the second lo_rows rows behind the first, in
+// fp32 in place; and x [M, H] with zeros for the tokens that do not count, in bf16 a second time lo_rows rows behind.
+hipError_t head_grad(int dtype, const float* z, int ldz, const float2* rows, const int64_t* labels, int M, int N, void* d, int lo_rows,
+                     const void* x, void* xs, int H, hipStream_t st);
+
+// ---- lists of tensors (tensors.hip)
+constexpr int LIST_CHUNK = 8192;         // elements that a workgroup takes at a time
+constexpr int CLIP_LIST = 64, ADAMW_LIST = 48;   // tensors of a launch: what fits a kernel's arguments, and a wave's lanes
+constexpr int CLIP_SLOTS = 1024;         // partial sums of squares
+// `head` elements lie in front of the first one at which all pointers are aligned for vectors; -1: there is none.  Chunk c of the
+// launch belongs to the last tensor with first <= c.
+struct ClipItem { const void* g; void* out; int64_t count; int32_t first; int16_t head, bf16; };
+struct ClipList { int n, chunks; ClipItem t[CLIP_LIST]; };
+struct AdamwItem { void* param; float* master; float* m; float* v; const void* g; int64_t count; float keep; int32_t first; int16_t head, param_bf16, grad_bf16, pad; };
+struct AdamwList { int n, chunks; AdamwItem t[ADAMW_LIST]; };
+// keep: 1 - lr * decay
+struct AdamwHyper { float beta1, rest1, beta2, rest2, eps, step_size, inv_sqrt_bc2; };   // rest: 1 - beta
+// slots[0 .. wgs-1] (+)= sums of squares; wgs <= CLIP_SLOTS workgroups
+hipError_t clip_squares(const ClipList& l, double* slots, int wgs, int add, hipStream_t st);
+// result = (norm, factor) of the `slots` sums
+hipError_t clip_result(const double* slots, int n_slots, float max_norm, float* result, hipStream_t st);
+// the same (where `result` is not null), and the clipped copies
+hipError_t clip_scale(const ClipList& l, const double* slots, int n_slots, float max_norm, float* result, hipStream_t st);
+hipError_t adamw(const AdamwList& l, const AdamwHyper& h, const float* factor, hipStream_t st);
 
 }  // namespace hh
