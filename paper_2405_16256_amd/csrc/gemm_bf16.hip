@@ -344,15 +344,21 @@ __global__ __launch_bounds__(512) void k_gemm_dma(DmaGroup grp, int full, int n_
 // k_gemm_dma's loop -> halves in order -> in turn: 16384x2048 51 -> 61 -> 44 us, 8192x4096 67 -> 58 -> 49, 12288x4096 71 -> 75 -> 64;
 // 16384x2112 48 -> 49 -> 49.  K 700 6144x16384 253 -> 246 -> 229.  What the longer prologue costs shows where the sums are short
 // and there is one round of tiles: 4096x4096 by 64 14.6 -> 15.2, by 512 24.4 -> 25.1.
+// PAIR: A's rows come in pairs, row grp.K + k behind row k, whose sum stands for one row in more bits than bf16 has (GemmDesc::pair).
+// A stage is then 32 rows of B, the 32 of A that they go with and the 32 second ones: B's fragments serve two MFMAs each, and a stage
+// takes three quarters of the requests and five sixths of the fragment reads of the same product over B stacked twice.
+template <bool PAIR>
 __global__ __launch_bounds__(512) void k_gemm_dma_tn(DmaGroup grp, int full, int n_items, float* __restrict__ partial) {
-    using DT = DmaTile<false, DHALF, 8>;
-    constexpr int TM = 4, TN = 2, PW = DT::PER_WAVE, HALF_BYTES = DT::BYTES;   // 2 instructions a wave, 16 KB
+    using DT = DmaTile<false, DHALF, 8>;                           // 2 instructions a wave, 16 KB
+    using DB = DmaTile<false, DHALF, 8, PAIR ? DK / 2 : DK>;
+    constexpr int TM = 4, TN = 2, PW = DT::PER_WAVE, PWB = DB::PER_WAVE, HALF_BYTES = DT::BYTES;
+    constexpr int KV = PAIR ? DK / 2 : DK, BF = KV / 16;           // rows of B in a stage, its k steps
     constexpr int B_LDS = DSTAGES * DSTAGE_BYTES;
     extern __shared__ __attribute__((aligned(1024))) char smem[];   // A [stage][half] | B [stage][half] | patches
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = (wave >> 2) * 64, wn = (wave & 3) * 32;          // in each half
-    const int nk_all = (grp.K + DK - 1) / DK;
+    const int nk_all = (grp.K + KV - 1) / KV;
     int prob, m0, n0, kbeg, nk, slot;                               // of a work item, as in k_gemm_dma
     int turn;                                                       // A's halves change places
     auto decode = [&](int item) {
@@ -375,27 +381,33 @@ __global__ __launch_bounds__(512) void k_gemm_dma_tn(DmaGroup grp, int full, int
 
     constexpr uint32_t OUT_OF_RANGE = 0x80000000u;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem) + wave * (PW * 1024);
+    const uint32_t ldsB = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem) + B_LDS + wave * (PWB * 1024);
     // A half's buffer begins at its first byte of the k tile asked for next, so that a lane's offset is the same in every k tile.
     struct Half { uint64_t at; int left; };   // left: elements up to the operand's end
     Half hA[2], hB[2];
-    uint32_t voA[PW], voB[PW], stepA, stepB;
+    uint32_t voA[PW], voB[PWB], stepA, stepB;
     // instruction p of a half; the last one moves on to the next k tile
-    auto dma_half = [&](Half& h, const uint32_t (&vo)[PW], uint32_t step, int lds, int p) {
+    auto dma_half = [&](Half& h, uint32_t vo, uint32_t step, uint32_t lds, bool last) {
         const i32x4 rs = {(int)(uint32_t)h.at, (int)(uint32_t)(h.at >> 32), max(h.left, 0) << 1, 0x00020000};
-        dma16(lds0 + lds + p * 1024, vo[p], rs);
-        if (p == PW - 1) {
+        dma16(lds, vo, rs);
+        if (last) {
             h.at += step;
             h.left -= (int)(step >> 1);
         }
     };
-    auto dma_a = [&](int st, int half, int p) { dma_half(hA[half], voA, stepA, st * DSTAGE_BYTES + half * HALF_BYTES, p); };
-    auto dma_b = [&](int st, int half, int p) { dma_half(hB[half], voB, stepB, B_LDS + st * DSTAGE_BYTES + half * HALF_BYTES, p); };
+    auto dma_a = [&](int st, int half, int p) { dma_half(hA[half], voA[p], stepA, lds0 + st * DSTAGE_BYTES + half * HALF_BYTES + p * 1024, p == PW - 1); };
+    auto dma_b = [&](int st, int half, int p) { dma_half(hB[half], voB[p], stepB, ldsB + st * DSTAGE_BYTES + half * HALF_BYTES + p * 1024, p == PWB - 1); };
     // point the DMA at the decoded tile and put its first two k tiles on their way
     auto start_tile = [&]() {
         const DmaProblem& g = grp.p[prob];
-        stepA = DT::kstep_bytes(g.lda); stepB = DT::kstep_bytes(g.ldb);
+        stepA = PAIR ? DB::kstep_bytes(g.lda) : DT::kstep_bytes(g.lda); stepB = DB::kstep_bytes(g.ldb);
 #pragma unroll
-        for (int i = 0; i < PW; i++) { voA[i] = DT::voff(wave, i, 0, g.lda); voB[i] = DT::voff(wave, i, 0, g.ldb); }
+        for (int i = 0; i < PW; i++) {
+            voA[i] = DT::voff(wave, i, 0, g.lda);
+            if (PAIR && wave * PW + i >= 4 * PW) voA[i] += (uint32_t)(grp.K - KV) * (uint32_t)g.lda * 2u;   // the second half of the rows
+        }
+#pragma unroll
+        for (int i = 0; i < PWB; i++) voB[i] = DB::voff(wave, i, 0, g.ldb);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const uint32_t skip_a = (uint32_t)(m0 + (h ^ turn) * DHALF) * 2u + (uint32_t)kbeg * stepA;
@@ -409,9 +421,9 @@ __global__ __launch_bounds__(512) void k_gemm_dma_tn(DmaGroup grp, int full, int
 #pragma unroll
                 for (int p = 0; p < PW; p++) dma_a(s, 0, p);
 #pragma unroll
-                for (int p = 0; p < PW; p++) dma_b(s, 0, p);
+                for (int p = 0; p < PWB; p++) dma_b(s, 0, p);
 #pragma unroll
-                for (int p = 0; p < PW; p++) dma_b(s, 1, p);
+                for (int p = 0; p < PWB; p++) dma_b(s, 1, p);
 #pragma unroll
                 for (int p = 0; p < PW; p++) dma_a(s, 1, p);
             }
@@ -435,35 +447,35 @@ __global__ __launch_bounds__(512) void k_gemm_dma_tn(DmaGroup grp, int full, int
                 for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
 
         // k tile 0 has landed, as in k_gemm_dma
-        if (fresh && nk > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * PW) : "memory");
+        if (fresh && nk > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (PW + PWB)) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         sync();
-        bf16x8 a[2][2][4], b[2][4];   // A: half, row block, k step; B: register set, k step
+        bf16x8 a[2][2][4], b[2][BF];   // A: half, row block, k step; B: register set, k step
         // fragment f of a half, in the order in which the MFMAs take them
         auto read_a = [&](int st, int half, int f) {
             a[half][f & 1][f >> 1] = DT::frag(smem + st * DSTAGE_BYTES + half * HALF_BYTES, wm + 32 * (f & 1), f >> 1);
         };
-        auto read_b = [&](int set, int st, int half, int f) { b[set][f] = DT::frag(smem + B_LDS + st * DSTAGE_BYTES + half * HALF_BYTES, wn, f); };
+        auto read_b = [&](int set, int st, int half, int f) { b[set][f] = DB::frag(smem + B_LDS + st * DSTAGE_BYTES + half * HALF_BYTES, wn, f); };
 #pragma unroll
         for (int f = 0; f < 8; f++) read_a(0, 0, f);
 #pragma unroll
-        for (int f = 0; f < 4; f++) read_b(0, 0, 0, f);
+        for (int f = 0; f < BF; f++) read_b(0, 0, 0, f);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         sync();
 
         // The 8 MFMAs of quadrant (ha, hb), B from register set `set`; meanwhile the fragments of a half that is needed later are read
         // and the two DMA instructions of one whose place is free are issued.
-        auto quadrant = [&](int ha, int hb, int set, auto read, int n_reads, auto dma, bool more) {
+        auto quadrant = [&](int ha, int hb, int set, auto read, int n_reads, auto dma, int n_dma, bool more) {
 #pragma unroll
             for (int q = 0; q < 8; q++) {
                 f32x16& c = acc[2 * ha + (q & 1)][hb];
-                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[set][q >> 1], a[ha][q & 1][q >> 1], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[set][(q >> 1) % BF], a[ha][q & 1][q >> 1], c, 0, 0, 0);
 #pragma unroll
                 for (int f = 0; f < 8; f++)
                     if (f < n_reads && f * 4 / n_reads == q) read(f);
 #pragma unroll
                 for (int p = 0; p < PW; p++)
-                    if (q == 4 * p + 2 && more) dma(p);
+                    if (p < n_dma && q == 4 * p + 2 && more) dma(p);
                 SB();
             }
         };
@@ -473,14 +485,14 @@ __global__ __launch_bounds__(512) void k_gemm_dma_tn(DmaGroup grp, int full, int
         auto stage = [&](auto parity, int kt) {
             constexpr int S = decltype(parity)::value, O = S ^ 1;
             const bool more = kt + 2 < nk;
-            quadrant(0, 0, S, [&](int f) { read_b(O, S, 1, f); }, 4, [&](int p) { dma_a(S, 0, p); }, more);
-            quadrant(0, 1, O, [&](int f) { read_a(S, 1, f); }, 8, [&](int p) { dma_b(S, 0, p); }, more);
-            if (more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(4 * PW) : "memory");
-            else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * PW) : "memory");
+            quadrant(0, 0, S, [&](int f) { read_b(O, S, 1, f); }, BF, [&](int p) { dma_a(S, 0, p); }, PW, more);
+            quadrant(0, 1, O, [&](int f) { read_a(S, 1, f); }, 8, [&](int p) { dma_b(S, 0, p); }, PWB, more);
+            if (more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (PW + PWB)) : "memory");
+            else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PW + PWB) : "memory");
             sync();
-            quadrant(1, 1, O, [&](int f) { read_a(O, 0, f); }, 8, [&](int p) { dma_b(S, 1, p); }, more);
-            quadrant(1, 0, S, [&](int f) { read_b(O, O, 0, f); }, 4, [&](int p) { dma_a(S, 1, p); }, more);
-            if (more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(4 * PW) : "memory");
+            quadrant(1, 1, O, [&](int f) { read_a(O, 0, f); }, 8, [&](int p) { dma_b(S, 1, p); }, PWB, more);
+            quadrant(1, 0, S, [&](int f) { read_b(O, O, 0, f); }, BF, [&](int p) { dma_a(S, 1, p); }, PW, more);
+            if (more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (PW + PWB)) : "memory");
             else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             sync();
         };
@@ -643,28 +655,30 @@ static int tail_shares(const GemmDesc& g, int tiles, int cus) {
 // Full rounds of one tile per compute unit run as one persistent workgroup per unit.  A last, partial round of R
 // tiles would leave most units idle, so it is cut along k into floor(units / R) shares per tile, which the same
 // workgroups take up after their whole tiles (fp32 partials in `ws`, summed in a fixed order by a small second kernel).
-template <int KIND, bool RES, bool SCORES>
+// FLAG: RES of NT and NN problems, PAIR of TN ones.
+template <int KIND, bool FLAG, bool SCORES>
 static auto dma_kernel() {
-    if constexpr (KIND == GEMM_TN) return &k_gemm_dma_tn;
-    else return &k_gemm_dma<KIND, RES, SCORES>;
+    if constexpr (KIND == GEMM_TN) return &k_gemm_dma_tn<FLAG>;
+    else return &k_gemm_dma<KIND, FLAG, SCORES>;
 }
-template <int KIND, bool RES = false, bool SCORES = false>
+template <int KIND, bool FLAG = false, bool SCORES = false>
 static hipError_t launch_dma(const GemmDesc* g, int n, hipStream_t st) {
     constexpr int LDS = DSTAGES * 2 * DSTAGE_BYTES + 8 * 4096;   // two stages + the epilogue patches of the 8 waves
     static std::atomic<uint64_t> lds_ok{0};
-    auto kern = dma_kernel<KIND, RES, SCORES>();
+    auto kern = dma_kernel<KIND, FLAG, SCORES>();
     const hipError_t e = allow_lds((const void*)kern, LDS, lds_ok);
     if (e != hipSuccess) return e;
     hipError_t ce = hipSuccess;
     const int NUM_CU = device_cus(ce);
     if (ce != hipSuccess) return ce;
     DmaGroup grp{};
-    grp.K = g[0].K;
+    constexpr bool PAIR = KIND == GEMM_TN && FLAG;
+    grp.K = PAIR ? g[0].K / 2 : g[0].K;
     int tiles = 0;
     for (int i = 0; i < DMA_MAX; i++) grp.first[i] = INT_MAX;
     for (int i = 0; i < n; i++) {
         const GemmDesc& q = g[i];
-        grp.p[i] = DmaProblem{(const bf16_t*)q.A, (const bf16_t*)q.B, q.C, (const bf16_t*)q.R, (uint32_t)extent_a(q), (uint32_t)extent_b(q, q.K),
+        grp.p[i] = DmaProblem{(const bf16_t*)q.A, (const bf16_t*)q.B, q.C, (const bf16_t*)q.R, (uint32_t)extent_a(q), (uint32_t)extent_b(q, grp.K),
                               q.lda, q.ldb, q.ldc, q.ldr, q.M, q.N, q.accumulate, tile_map(q.M, q.N, DTILE, DTILE)};
         grp.first[i] = tiles;
         tiles += grp.p[i].map.tiles();
@@ -969,8 +983,11 @@ static hipError_t launch_tiles256(const GemmDesc* g, int n, hipStream_t st) {
     switch (g[0].kind) {
         case GEMM_NT: return res ? launch_dma<GEMM_NT, true>(g, n, st) : launch_dma<GEMM_NT>(g, n, st);
         case GEMM_NN: return res ? launch_dma<GEMM_NN, true>(g, n, st) : launch_dma<GEMM_NN>(g, n, st);
-        default: return launch_dma<GEMM_TN>(g, n, st);
+        default: break;
     }
+    bool pair = true;
+    for (int i = 0; i < n; i++) pair = pair && g[i].pair;
+    return pair ? launch_dma<GEMM_TN, true>(g, n, st) : launch_dma<GEMM_TN>(g, n, st);
 }
 template <bool BWD>
 static hipError_t launch_variant(const GemmDesc* g, int n, const Plan& p, hipStream_t st) {
@@ -1062,6 +1079,7 @@ static hipError_t check(const GemmDesc& g) {
     // 32-bit byte offsets, which run past the end by at most the 256 rows of a tile
     if (a_bytes >= (1L << 32) - (1L << 25) || b_bytes >= (1L << 32) - (1L << 25)) return hipErrorInvalidValue;
     if (g.lda > MAX_LD || g.ldb > MAX_LD || a_bytes + 512L * g.lda >= (1L << 32) || b_bytes + 512L * g.ldb >= (1L << 32)) return hipErrorInvalidValue;
+    if (g.pair && (g.kind != GEMM_TN || g.K % 2 || g.b_rows || g.micro > 1)) return hipErrorInvalidValue;
     if (g.b_rows && (g.k1 || g.b_rows < 0 || g.b_rows > (g.kind == GEMM_NT ? g.N : g.K))) return hipErrorInvalidValue;
     if (g.scores) {
         const GemmScores& s = *g.scores;
@@ -1253,9 +1271,11 @@ static hipError_t gemm_scores(const GemmDesc& g, hipStream_t st) {
         const double u = rounds_us(VARIANTS[v], tiles_of(g, VARIANTS[v]), nk) + VARIANTS[v].t0;
         if (u < t) { t = u; best = v; }
     }
-    if (best == V_64x128) return launch_ring_scores<64, 128, 2, 2, 3>(g, st);
-    if (best == V_128x256) return launch_ring_scores<128, 256, 2, 4, 3>(g, st);
-    return launch_dma<GEMM_NT, false, true>(&g, 1, st);
+    switch (best) {
+        case V_64x128: return launch_ring_scores<64, 128, 2, 2, 3>(g, st);
+        case V_128x256: return launch_ring_scores<128, 256, 2, 4, 3>(g, st);
+        default: return launch_dma<GEMM_NT, false, true>(&g, 1, st);
+    }
 }
 
 hipError_t gemm_bf16(const GemmDesc* g, int n, hipStream_t st) {

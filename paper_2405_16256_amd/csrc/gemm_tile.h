@@ -66,9 +66,11 @@ __device__ __forceinline__ void dma16(uint32_t lds_addr, uint32_t voff, i32x4 rs
 //   otherwise (k strided):       LDS [k][row], 64-byte slots XOR-swizzled by the k index; fragments come out with the
 //      transposing ds_read_b64_tr_b16.
 // Either way lane l of a fragment holds row (l % 32), k = 16*step + 8*(l/32) .. +7.
-template <bool KC, int ROWS, int NW>
+// KV: k values of a stage (k strided).
+template <bool KC, int ROWS, int NW, int KV = DK>
 struct DmaTile {
-    static constexpr int BYTES = ROWS * DK * 2;
+    static_assert(KV == DK || !KC, "a k-contiguous row is a whole line");
+    static constexpr int BYTES = ROWS * KV * 2;
     static constexpr int PER_WAVE = BYTES / 1024 / NW;   // DMA instructions of 1 KB a wave issues per stage
     static_assert(PER_WAVE * NW * 1024 == BYTES, "the tile must split evenly over the waves");
     static constexpr int PITCH = ROWS * 2;               // bytes of a k row (k strided)
@@ -91,7 +93,7 @@ struct DmaTile {
             return ((uint32_t)k * (uint32_t)ld + (uint32_t)row0) * 2u + (uint32_t)lbyte;
         }
     }
-    __device__ static __forceinline__ uint32_t kstep_bytes(int ld) { return KC ? DK * 2u : (uint32_t)DK * (uint32_t)ld * 2u; }
+    __device__ static __forceinline__ uint32_t kstep_bytes(int ld) { return KC ? DK * 2u : (uint32_t)KV * (uint32_t)ld * 2u; }
     // fragment of 32 rows starting at rb, k step kk (0..3)
     __device__ static __forceinline__ bf16x8 frag(const char* lds, int rb, int kk) {
         const int l = threadIdx.x & 63;

@@ -416,7 +416,7 @@ GemmDesc hh::desc(int kind, int M, int N, int K, const void* A, int lda, const v
     g.R = R; g.ldr = ldr; g.out_f32 = out_f32; g.accumulate = acc; g.ws = nullptr; g.ws_bytes = 0;
     g.B1 = g.B2 = nullptr; g.k1 = g.k2 = 0;
     g.fuse = GemmFuse{}; g.split = nullptr; g.norm = nullptr; g.scores = nullptr;
-    g.b_rows = 0; g.micro = 1; g.each = nullptr;
+    g.b_rows = 0; g.pair = 0; g.micro = 1; g.each = nullptr;
     return g;
 }
 

@@ -46,7 +46,7 @@ static HeadPlan head_plan(const hh_head_cfg* c, bool step) {
     p.block = split_evenly(p.T, (int)std::max<long>(most, 1));
     p.piece = p.block;
     if (bf && step) {
-        const long rows = std::max<long>(256, (1L << 28) / (4L * p.ld) / 256 * 256);
+        const long rows = std::max<long>(256, (1L << 29) / (4L * p.ld) / 256 * 256);
         p.piece = (int)std::min<long>(p.block, rows);
     }
     size_t off = 0;
@@ -117,6 +117,7 @@ static int head_run(hh_ctx* ctx, const HeadPlan& p, const void* x, const void* w
             if (n == 4) { HIP_TRY(tgemm(ctx, p.dt, g, n, st)); n = 0; }
             g[n++] = desc(GEMM_TN, std::min(most, V - v0), H, bf ? 2 * T : T, at(d, (size_t)v0 * es), p.ld, xs, H, dw + (size_t)v0 * H, H,
                           nullptr, 0, 1, accumulate || t0 > 0);
+            g[n - 1].pair = bf;
         }
         HIP_TRY(tgemm(ctx, p.dt, g, n, st));
     }

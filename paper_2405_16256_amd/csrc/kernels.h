@@ -54,6 +54,7 @@ struct GemmDesc {
     int M, N, K;
     const void* A; int lda;
     const void* B; int ldb;
+    int pair;                // TN (bf16): row K/2 + k of A is what row k lacks of its value, and row K/2 + k of B is row k again
     int b_rows;              // rows of B that are there (0: as many as the product has); the others read as zeros
     void* C; int ldc;
     const void* R; int ldr;  // optional residual in the storage dtype, added before rounding (NULL: none)
