@@ -63,7 +63,7 @@ int hh_head_step(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void 
  * out == NULL counts a tensor without a clipped copy; out may be g.  Squares are formed and added in fp64, so gradients of any
  * size can be summed.  A norm that is not finite gives the factor NaN.  Pointers need the alignment of their type
  * alone (16 bytes for all pointers of a tensor, or the same distance from it, is faster).  tensors is a HOST array, read during the call;
- * n may be 0, and so may a count, whose pointers are not looked at.
+ * n may be 0, and so may a count, whose pointers are not looked at; a count is at most 2^34.
  * result: device, fp32: result[0] = norm, result[1] = factor. */
 typedef struct {
     const void *g;    /* gradient, in `dtype` */

@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <climits>
 
 #include "ctx.h"
 #include "kernels.h"
@@ -154,9 +153,9 @@ static int lead(const Typed* p, int n, int vec) {
     }
     return -1;
 }
-static long chunks_of(int64_t count, int head) {
+static long chunks_of(int64_t count, int head, int chunk) {
     const int64_t body = std::max<int64_t>(count - std::max(head, 0), 0);
-    return std::max<long>(1, (long)((body + LIST_CHUNK - 1) / LIST_CHUNK));
+    return std::max<long>(1, (long)((body + chunk - 1) / chunk));
 }
 static int check_item(int i, const char* name, const void* p, size_t es) {
     if (!p) return fail(HH_ERR_INVALID_ARG, "tensors[%d].%s is NULL", i, name);
@@ -170,10 +169,12 @@ static int check_list(int n, const void* tensors) {
 }
 static bool is_dtype(int d) { return d == HH_F32 || d == HH_BF16; }
 static size_t size_of(int d) { return d == HH_BF16 ? 2 : 4; }
-constexpr int64_t MAX_COUNT = (int64_t)1 << 40;   // chunks are counted in 32 bits
+constexpr int64_t MAX_COUNT = (int64_t)1 << 34;
+constexpr long MAX_CHUNKS = (1L << 24) - 8;        // 256 threads each, below 2^32 in a launch
+static_assert(MAX_COUNT / ADAMW_CHUNK + 1 < MAX_CHUNKS && MAX_COUNT / CLIP_CHUNK + 1 < MAX_CHUNKS, "a tensor fits a launch");
 
 // Fills lists of up to MAX tensors and hands each of them to `launch`.
-template <typename List, int MAX, typename Tensor, typename Fill, typename Launch>
+template <typename List, int MAX, int CHUNK, typename Tensor, typename Fill, typename Launch>
 static int for_lists(int n, const Tensor* tensors, Fill fill, Launch launch) {
     List l;
     l.n = l.chunks = 0;
@@ -181,8 +182,8 @@ static int for_lists(int n, const Tensor* tensors, Fill fill, Launch launch) {
         if (tensors[i].count == 0) continue;
         auto& t = l.t[l.n];
         fill(tensors[i], t);
-        const long c = chunks_of(tensors[i].count, t.head);
-        if (l.n && l.chunks + c > INT_MAX / 2) {
+        const long c = chunks_of(tensors[i].count, t.head, CHUNK);
+        if (l.n && l.chunks + c > MAX_CHUNKS) {
             TRY(launch(l));
             l.t[0] = t;
             l.n = l.chunks = 0;
@@ -212,7 +213,7 @@ extern "C" int hh_grad_clip(hh_ctx* ctx, int n, const hh_clip_tensor* tensors, f
     for (int i = 0; i < n; i++) {
         const hh_clip_tensor& t = tensors[i];
         if (!is_dtype(t.dtype)) return fail(HH_ERR_INVALID_ARG, "tensors[%d].dtype %d is not HH_F32/HH_BF16", i, t.dtype);
-        if (t.count < 0 || t.count > MAX_COUNT) return fail(HH_ERR_INVALID_ARG, "tensors[%d].count is negative or exceeds 2^40", i);
+        if (t.count < 0 || t.count > MAX_COUNT) return fail(HH_ERR_INVALID_ARG, "tensors[%d].count is negative or exceeds 2^34", i);
         if (t.count == 0) continue;
         TRY(check_item(i, "g", t.g, size_of(t.dtype)));
         if (t.out) TRY(check_item(i, "out", t.out, size_of(t.dtype)));
@@ -221,7 +222,7 @@ extern "C" int hh_grad_clip(hh_ctx* ctx, int n, const hh_clip_tensor* tensors, f
     if (!ctx) return fail(HH_ERR_INVALID_ARG, "ctx is NULL");
     const hipStream_t st = (hipStream_t)stream;
     double* const slots = (double*)workspace;
-    auto lists = [&](auto launch) { return for_lists<ClipList, CLIP_LIST>(n, tensors, fill_clip, launch); };
+    auto lists = [&](auto launch) { return for_lists<ClipList, CLIP_LIST, CLIP_CHUNK>(n, tensors, fill_clip, launch); };
     double bytes = 0.0;
     TRY(lists([&](const ClipList& l) -> int {
         most = std::max<long>(most, l.chunks);
@@ -273,7 +274,7 @@ extern "C" int hh_adamw_step(hh_ctx* ctx, const hh_adamw_cfg* cfg, int n, const 
     for (int i = 0; i < n; i++) {
         const hh_adamw_tensor& t = tensors[i];
         if (!is_dtype(t.param_dtype) || !is_dtype(t.grad_dtype)) return fail(HH_ERR_INVALID_ARG, "tensors[%d] has a dtype that is not HH_F32/HH_BF16", i);
-        if (t.count < 0 || t.count > MAX_COUNT) return fail(HH_ERR_INVALID_ARG, "tensors[%d].count is negative or exceeds 2^40", i);
+        if (t.count < 0 || t.count > MAX_COUNT) return fail(HH_ERR_INVALID_ARG, "tensors[%d].count is negative or exceeds 2^34", i);
         if (!(t.decay >= 0.f)) return fail(HH_ERR_INVALID_ARG, "tensors[%d].decay must be >= 0", i);
         if (t.count == 0) continue;
         const bool pb = t.param_dtype == HH_BF16;
@@ -290,8 +291,8 @@ extern "C" int hh_adamw_step(hh_ctx* ctx, const hh_adamw_cfg* cfg, int n, const 
     const AdamwHyper h{(float)cfg->beta1, (float)(1.0 - cfg->beta1), (float)cfg->beta2, (float)(1.0 - cfg->beta2), (float)cfg->eps, (float)(cfg->lr / bc1), (float)(1.0 / std::sqrt(bc2))};
     auto fill = [&](const hh_adamw_tensor& q, AdamwItem& t) { fill_adamw(q, cfg->lr, t); };
     Traced t_(ctx, st, HH_TRACE_ELEMENTWISE, 1, bytes);
-    return for_lists<AdamwList, ADAMW_LIST>(n, tensors, fill, [&](const AdamwList& l) -> int {
-        HIP_TRY(adamw(l, h, factor, st));
+    return for_lists<AdamwList, ADAMW_LIST, ADAMW_CHUNK>(n, tensors, fill, [&](const AdamwList& l) -> int {
+        HIP_TRY(adamw(l, h, factor, bytes > (double)LIST_CACHE, st));
         return HH_OK;
     });
 }

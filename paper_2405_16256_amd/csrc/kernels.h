@@ -155,7 +155,9 @@ hipError_t head_grad(int dtype, const float* z, int ldz, const float2* rows, con
                      const void* x, void* xs, int H, hipStream_t st);
 
 // ---- lists of tensors (tensors.hip)
-constexpr int LIST_CHUNK = 8192;         // elements that a workgroup takes at a time
+constexpr int CLIP_CHUNK = 8192, ADAMW_CHUNK = 2048;   // elements that a workgroup takes at a time
+// What a launch reads and writes leaves nothing in the last-level cache for the next one where it is more than this.
+constexpr size_t LIST_CACHE = (size_t)256 << 20;
 constexpr int CLIP_LIST = 64, ADAMW_LIST = 48;   // tensors of a launch: what fits a kernel's arguments, and a wave's lanes
 constexpr int CLIP_SLOTS = 1024;         // partial sums of squares
 // `head` elements lie in front of the first one at which all pointers are aligned for vectors; -1: there is none.  Chunk c of the
@@ -172,6 +174,7 @@ hipError_t clip_squares(const ClipList& l, double* slots, int wgs, int add, hipS
 hipError_t clip_result(const double* slots, int n_slots, float max_norm, float* result, hipStream_t st);
 // the same (where `result` is not null), and the clipped copies
 hipError_t clip_scale(const ClipList& l, const double* slots, int n_slots, float max_norm, float* result, hipStream_t st);
-hipError_t adamw(const AdamwList& l, const AdamwHyper& h, const float* factor, hipStream_t st);
+// stream: the tensors of all launches together are past LIST_CACHE
+hipError_t adamw(const AdamwList& l, const AdamwHyper& h, const float* factor, bool stream, hipStream_t st);
 
 }  // namespace hh
