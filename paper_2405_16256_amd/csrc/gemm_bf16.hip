@@ -34,6 +34,7 @@
 #include <climits>
 #include <cstdio>
 #include <cstring>
+#include <iterator>
 
 #include "gemm_ring.h"
 #include "gemm_scores.h"
@@ -346,12 +347,16 @@ __global__ __launch_bounds__(512) void k_gemm_dma(DmaGroup grp, int full, int n_
 // and there is one round of tiles: 4096x4096 by 64 14.6 -> 15.2, by 512 24.4 -> 25.1.
 // PAIR: A's rows come in pairs, row grp.K + k behind row k, whose sum stands for one row in more bits than bf16 has (GemmDesc::pair).
 // A stage is then 32 rows of B, the 32 of A that they go with and the 32 second ones: B's fragments serve two MFMAs each, and a stage
-// takes three quarters of the requests and five sixths of the fragment reads of the same product over B stacked twice.
+// takes three quarters of the requests and five sixths of the fragment reads of the same product over B stacked twice: 32000x4096 over
+// 2 x 2048 rows 864 -> 817 us, x 12288 over 2 x 4096 with += 5168 -> 4973.  C goes past the caches: it is the gradient of a whole
+// vocabulary, and 256 MB of its dirty lines in the last-level cache hold up whoever reads next (a step of 64 tokens over 32000x4096
+// 275 -> 212 us, of 333 459 -> 437, of 2048 1834 -> 1816).
 template <bool PAIR>
 __global__ __launch_bounds__(512) void k_gemm_dma_tn(DmaGroup grp, int full, int n_items, float* __restrict__ partial) {
     using DT = DmaTile<false, DHALF, 8>;                           // 2 instructions a wave, 16 KB
     using DB = DmaTile<false, DHALF, 8, PAIR ? DK / 2 : DK>;
     constexpr int TM = 4, TN = 2, PW = DT::PER_WAVE, PWB = DB::PER_WAVE, HALF_BYTES = DT::BYTES;
+    constexpr int PAST_CACHES = 2;                                 // a store's nt bit
     constexpr int KV = PAIR ? DK / 2 : DK, BF = KV / 16;           // rows of B in a stage, its k steps
     constexpr int B_LDS = DSTAGES * DSTAGE_BYTES;
     extern __shared__ __attribute__((aligned(1024))) char smem[];   // A [stage][half] | B [stage][half] | patches
@@ -566,7 +571,7 @@ __global__ __launch_bounds__(512) void k_gemm_dma_tn(DmaGroup grp, int full, int
                     const float4 v = *reinterpret_cast<const float4*>(patch + rr * 128 + ((c_r ^ ((rr >> 1) & 7)) << 4));
                     const i32x4 o = {__float_as_int(v.x + add[j][t].x), __float_as_int(v.y + add[j][t].y), __float_as_int(v.z + add[j][t].z),
                                      __float_as_int(v.w + add[j][t].w)};
-                    __builtin_amdgcn_raw_buffer_store_b128(o, rsC, off_c[j][t], 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(o, rsC, off_c[j][t], 0, PAIR ? PAST_CACHES : 0);
                 }
             }
         }
@@ -837,6 +842,11 @@ static constexpr Variant VARIANTS[V_COUNT] = {
     {256, 256, 1, false, 0.97, 5.44, 1.587, 1.639},
 };
 static constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8};
+// The input gradient of an output projection has k loops of hundreds of stages over a vocabulary and few tiles: more splits to choose
+// from.  700x1024x50048: 8 shares of 24 tiles 115 us, 10 shares 105; 333x4096x32000: 4 shares of 48 tiles 114, 5 shares 112.
+static constexpr int VOCAB_SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24};
+struct Splits { const int *from, *to; const int* begin() const { return from; } const int* end() const { return to; } };
+static Splits splits_of(const GemmDesc& g) { return g.b_rows ? Splits{std::begin(VOCAB_SPLITS), std::end(VOCAB_SPLITS)} : Splits{std::begin(SPLITS), std::end(SPLITS)}; }
 
 // Time of a k stage in a last round of `busy` workgroups, one per CU.  Where each CU holds one workgroup at most anyway,
 // loops of more than 64 stages run the longer towards t_full the more CUs are busy (the power limit and the traffic
@@ -892,7 +902,7 @@ static Plan plan_one(const GemmDesc& g, bool whole_only) {
             if (t < best.t) best = Plan{V_DMA, {1}, {0}, t};
             continue;
         }
-        for (const int s : SPLITS) {
+        for (const int s : splits_of(g)) {
             if (!may_split(g, q, s)) break;
             double t = std::max(rounds_us(q, tiles * s, (double)nk / s), floor);
             if (s > 1) t += 3.0 + reduce_us(g, q, s);
@@ -966,8 +976,8 @@ static Plan plan(const GemmDesc* g, int n, bool whole_only) {
     struct Slot { PlanKey key; Plan plan; };
     static thread_local Slot slots[256];
     PlanKey k{};
-    k.n = n; k.whole = whole_only; k.ws = g[0].ws ? g[0].ws_bytes : 0;
-    uint32_t h = (uint32_t)n * 2u + whole_only;
+    k.n = n; k.whole = whole_only + (g[0].b_rows ? 2 : 0); k.ws = g[0].ws ? g[0].ws_bytes : 0;
+    uint32_t h = (uint32_t)n * 4u + (uint32_t)k.whole;
     for (int i = 0; i < n; i++) {
         const int v[4] = {g[i].kind, g[i].M, g[i].N, g[i].K};
         for (int j = 0; j < 4; j++) { k.sizes[i][j] = v[j]; h = (h ^ (uint32_t)v[j]) * 0x9E3779B1u; h ^= h >> 15; }
@@ -1241,7 +1251,9 @@ static hipError_t micro_launches(const GemmDesc* g, int n, const Route& r, L lau
     return e;
 }
 
-// Scores: the variants whose waves own 64 columns, uncut.
+// Scores: tiles whose waves own 64 columns, uncut, by the model's times.  Up to 64 rows the weight is read once and nothing else
+// counts: tiles of 64 columns have twice the workgroups and three stages on their way instead of two (1x4096x32000 59.7 -> 54.5 us,
+// 5x11712x12379 90.7 -> 64.3), unless k is short (1x1024x50001 22.2 -> 24.0).
 template <int BM, int BN, int WM, int WN, int NS>
 static hipError_t launch_ring_scores(const GemmDesc& g, hipStream_t st) {
     constexpr int LDS = NS * (BM + BN) * DK * 2;
@@ -1265,6 +1277,7 @@ static hipError_t launch_ring_scores(const GemmDesc& g, hipStream_t st) {
 }
 static hipError_t gemm_scores(const GemmDesc& g, hipStream_t st) {
     const int nk = g.K / DK;
+    if (g.M <= 64 && g.K >= 2048) return launch_ring_scores<64, 64, 2, 1, 4>(g, st);
     int best = V_DMA;
     double t = tiles_of(g, VARIANTS[V_DMA]) < 64 ? 1e30 : dma_us(tiles_of(g, VARIANTS[V_DMA]), nk, 0.0, false);
     for (const int v : {V_64x128, V_128x256}) {

@@ -158,7 +158,7 @@ hipError_t head_grad(int dtype, const float* z, int ldz, const float2* rows, con
 constexpr int CLIP_CHUNK = 8192, ADAMW_CHUNK = 2048;   // elements that a workgroup takes at a time
 // What a launch reads and writes leaves nothing in the last-level cache for the next one where it is more than this.
 constexpr size_t LIST_CACHE = (size_t)256 << 20;
-constexpr int CLIP_LIST = 64, ADAMW_LIST = 48;   // tensors of a launch: what fits a kernel's arguments, and a wave's lanes
+constexpr int CLIP_LIST = 112, ADAMW_LIST = 56;   // tensors of a launch: what fits a kernel's arguments (4 KB), two for each lane of a wave at most
 constexpr int CLIP_SLOTS = 1024;         // partial sums of squares
 // `head` elements lie in front of the first one at which all pointers are aligned for vectors; -1: there is none.  Chunk c of the
 // launch belongs to the last tensor with first <= c.
@@ -166,6 +166,7 @@ struct ClipItem { const void* g; void* out; int64_t count; int32_t first; int16_
 struct ClipList { int n, chunks; ClipItem t[CLIP_LIST]; };
 struct AdamwItem { void* param; float* master; float* m; float* v; const void* g; int64_t count; float keep; int32_t first; int16_t head, param_bf16, grad_bf16, pad; };
 struct AdamwList { int n, chunks; AdamwItem t[ADAMW_LIST]; };
+static_assert(sizeof(ClipList) + 32 <= 4096 && sizeof(AdamwList) + sizeof(float) * 16 <= 4096, "kernel arguments");
 // keep: 1 - lr * decay
 struct AdamwHyper { float beta1, rest1, beta2, rest2, eps, step_size, inv_sqrt_bc2; };   // rest: 1 - beta
 // slots[0 .. wgs-1] (+)= sums of squares; wgs <= CLIP_SLOTS workgroups

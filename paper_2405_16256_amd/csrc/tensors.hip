@@ -11,10 +11,22 @@
 
 namespace hh {
 
-// The tensor of chunk c: `first` is the lane's own entry (INT_MAX past the last tensor).
-__device__ __forceinline__ int tensor_of(int c, int first) {
-    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(first <= c)) - 1);
-}
+// Where the tensors of a list begin: the lane's own entries (INT_MAX past the last one); the tensor of chunk c.
+template <typename List, int MAX>
+struct Begins {
+    static_assert(MAX <= 2 * WAVE, "two entries a lane");
+    int first[MAX > WAVE ? 2 : 1];
+    __device__ __forceinline__ explicit Begins(const List& l) {
+        const int lane = threadIdx.x & 63;
+        first[0] = lane < l.n ? l.t[lane].first : INT_MAX;
+        if constexpr (MAX > WAVE) first[1] = lane + WAVE < l.n ? l.t[lane + WAVE].first : INT_MAX;
+    }
+    __device__ __forceinline__ int tensor_of(int c) const {
+        int n = __popcll(__ballot(first[0] <= c));
+        if constexpr (MAX > WAVE) n += __popcll(__ballot(first[1] <= c));
+        return __builtin_amdgcn_readfirstlane(n - 1);
+    }
+};
 
 // The elements of a chunk of CHUNK: [beg, end) in vectors of VN, beg aligned, and [s0, s1), [s2, s3) one by one.
 template <int VN, int CHUNK>
@@ -85,10 +97,10 @@ __device__ __forceinline__ double block_sum_f64(double v, double* red) {
 
 __global__ __launch_bounds__(256) void k_clip_squares(ClipList l, double* __restrict__ slots, int add) {
     __shared__ double red[4];
-    const int lane = threadIdx.x & 63, first = lane < l.n ? l.t[lane].first : INT_MAX;
+    const Begins<ClipList, CLIP_LIST> begins(l);
     double acc = 0.0;
     for (int c = (int)blockIdx.x; c < l.chunks; c += (int)gridDim.x) {
-        const ClipItem& t = l.t[tensor_of(c, first)];
+        const ClipItem& t = l.t[begins.tensor_of(c)];
         if (t.bf16) acc += squares((const bf16_t*)t.g, t.count, t.head, c - t.first);
         else acc += squares((const float*)t.g, t.count, t.head, c - t.first);
     }
@@ -146,10 +158,10 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipList l, const double* __
     __shared__ double red[4];
     const float2 r = norm_and_factor(slots, n_slots, max_norm, red);
     if (result && blockIdx.x == 0 && threadIdx.x == 0) { result[0] = r.x; result[1] = r.y; }
-    const int lane = threadIdx.x & 63, first = lane < l.n ? l.t[lane].first : INT_MAX;
+    const Begins<ClipList, CLIP_LIST> begins(l);
     const int c = ((int)(gridDim.x >> 3) - 1 - (int)(blockIdx.x >> 3)) * 8 + (int)(blockIdx.x & 7);
     if (c >= l.chunks) return;
-    const ClipItem& t = l.t[tensor_of(c, first)];
+    const ClipItem& t = l.t[begins.tensor_of(c)];
     if (!t.out) return;
     if (t.bf16) scaled((const bf16_t*)t.g, (bf16_t*)t.out, r.y, t.count, t.head, c - t.first);
     else scaled((const float*)t.g, (float*)t.out, r.y, t.count, t.head, c - t.first);
@@ -241,8 +253,9 @@ template <bool PAST>
 __global__ __launch_bounds__(256) void k_adamw(AdamwList l, AdamwHyper h, const float* __restrict__ factor) {
     const float f = factor ? *factor : 1.f;
     if (!(fabsf(f) < INFINITY)) return;   // gradients that are not finite: nothing changes
-    const int lane = threadIdx.x & 63, first = lane < l.n ? l.t[lane].first : INT_MAX, c = (int)blockIdx.x;
-    const AdamwItem& t = l.t[tensor_of(c, first)];
+    const Begins<AdamwList, ADAMW_LIST> begins(l);
+    const int c = (int)blockIdx.x;
+    const AdamwItem& t = l.t[begins.tensor_of(c)];
     const int64_t chunk = c - t.first;
     if (t.param_bf16) {
         if (t.grad_bf16) update<true, true, PAST>(t, h, f, chunk);
