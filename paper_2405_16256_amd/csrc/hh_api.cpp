@@ -34,6 +34,7 @@ hipError_t attn_f32_bwd(const void* qkv, int ld, const void* o, const void* dout
 
 hipError_t gemm(int dtype, const GemmDesc* g, int n, hipStream_t st) {
     if (dtype == DT_BF16) return gemm_bf16(g, n, st);
+    if (n == 1 && g[0].long_k) return gemm_f32_long_k(g[0], st);
     // the later segments of B one after the other behind the group, each adding to what the ones before it have left in C
     GemmDesc q[4];
     if (n < 1 || n > 4) return hipErrorInvalidValue;
@@ -345,7 +346,11 @@ extern "C" int hh_ctx_reserve(hh_ctx* ctx, const hh_layer_cfg* cfg) {
         HIP_TRY(call);                           \
     } while (0)
 static double attn_flop(const Dims& d) { return 4.0 * d.d * d.B * d.nh * ((double)d.S * (d.S + 1) / 2); }
-static double gemm_flop(const GemmDesc& g) { return 2.0 * g.M * g.N * g.K * g.micro; }
+// (rows of B that are not there and second terms of A are no model flops)
+static double gemm_flop(const GemmDesc& g) {
+    const int N = g.b_rows && g.kind == GEMM_NT ? g.b_rows : g.N, K = g.b_rows && g.kind == GEMM_NN ? g.b_rows : g.pair ? g.K / 2 : g.K;
+    return 2.0 * g.M * N * K * g.micro;
+}
 static void gemm_scratch(const hh_ctx* ctx, GemmDesc& g) { g.ws = ctx->gemm_ws; g.ws_bytes = ctx->gemm_ws ? GEMM_WS_BYTES : 0; g.ws_room = ctx->gemm_room; }
 // A group of GEMMs in one call.  Where they share a launch it is bracketed once and its time shared out to the members by
 // their flops; members with launches of their own are traced (and launched, in the same way) one by one.
@@ -416,7 +421,7 @@ GemmDesc hh::desc(int kind, int M, int N, int K, const void* A, int lda, const v
     g.R = R; g.ldr = ldr; g.out_f32 = out_f32; g.accumulate = acc; g.ws = nullptr; g.ws_bytes = 0;
     g.B1 = g.B2 = nullptr; g.k1 = g.k2 = 0;
     g.fuse = GemmFuse{}; g.split = nullptr; g.norm = nullptr; g.scores = nullptr;
-    g.b_rows = 0; g.pair = 0; g.micro = 1; g.each = nullptr;
+    g.b_rows = 0; g.pair = g.long_k = 0; g.micro = 1; g.each = nullptr;
     return g;
 }
 

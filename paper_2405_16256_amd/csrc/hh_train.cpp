@@ -57,7 +57,7 @@ static HeadPlan head_plan(const hh_head_cfg* c, bool step) {
         p.d = bf ? take((size_t)p.block * p.ld * 4) : p.z;
         p.xs = take((size_t)p.block * p.H * 4);
     }
-    p.gemm_ws = take(bf && step ? GEMM_WS_BYTES : 0);
+    p.gemm_ws = take(step ? GEMM_WS_BYTES : 0);
     p.total = off;
     return p;
 }
@@ -80,7 +80,7 @@ static int head_run(hh_ctx* ctx, const HeadPlan& p, const void* x, const void* w
     const bool bf = p.dt == DT_BF16, step = dx != nullptr;
     const size_t es = dt_size(p.dt);
     const int H = p.H, V = p.V;
-    ctx->gemm_ws = bf && step ? at(ws, p.gemm_ws) : nullptr;
+    ctx->gemm_ws = step ? at(ws, p.gemm_ws) : nullptr;
     ctx->gemm_room = 0;
     float2* const stats = (float2*)at(ws, p.stats);
     float2* const rows = step ? (float2*)at(ws, p.rows) : nullptr;
@@ -110,6 +110,11 @@ static int head_run(hh_ctx* ctx, const HeadPlan& p, const void* x, const void* w
         int n = 0;
         g[n] = desc(GEMM_NN, T, H, p.ld, d, p.ld, w, H, at(dx, (size_t)t0 * H * es), H);
         g[n++].b_rows = V;
+        if (!bf && gemm_f32_long_k_better(T, H, p.ld)) {
+            g[0].long_k = 1;
+            HIP_TRY(tgemm(ctx, p.dt, g, n, st));
+            n = 0;
+        }
         // fp32 sums of 2^31 bytes and more in pieces of the vocabulary
         const int most = (int)std::min<long>(V, std::max<long>(256, ((1L << 31) - 1) / (4L * H) / 256 * 256));
         for (int v0 = 0; v0 < V; v0 += most) {

@@ -55,6 +55,7 @@ struct GemmDesc {
     const void* A; int lda;
     const void* B; int ldb;
     int pair;                // TN (bf16): row K/2 + k of A is what row k lacks of its value, and row K/2 + k of B is row k again
+    int long_k;              // fp32: gemm_f32_long_k takes it
     int b_rows;              // rows of B that are there (0: as many as the product has); the others read as zeros
     void* C; int ldc;
     const void* R; int ldr;  // optional residual in the storage dtype, added before rounding (NULL: none)
@@ -83,6 +84,10 @@ void* static_scratch(int device);             // that address (null before a suc
 // Up to 4 problems (8 weight gradients in bf16) of which none reads what another writes, either all NT or none; they share launches where that is
 // predicted to be faster.
 hipError_t gemm(int dtype, const GemmDesc* g, int n, hipStream_t st);
+// One fp32 NN problem of a long k cut along it (gemm_f32_long_k.hip; needs `ws`, nothing added, no segments or micro-batches), and
+// whether that is better.
+hipError_t gemm_f32_long_k(const GemmDesc& g, hipStream_t st);
+bool gemm_f32_long_k_better(int M, int N, int K);
 // Whether all launches of these problems (bf16) are the ring kernel's, and if so: the bytes of partial sums that the largest of
 // those launches keeps, its workgroups, and the largest tile.
 struct RingUse { size_t partial; long workgroups; int tile; };
