@@ -1093,7 +1093,7 @@ static hipError_t check(const GemmDesc& g) {
     if (g.b_rows && (g.k1 || g.b_rows < 0 || g.b_rows > (g.kind == GEMM_NT ? g.N : g.K))) return hipErrorInvalidValue;
     if (g.scores) {
         const GemmScores& s = *g.scores;
-        if (g.kind != GEMM_NT || g.K % 64 || g.R || g.fuse.kind || g.norm || g.micro > 1 || !s.stats || !s.labels) return hipErrorInvalidValue;
+        if (g.kind != GEMM_NT || g.K % 64 || g.R || g.fuse.kind || g.norm || g.micro > 1 || (!s.stats && !s.z) || (s.stats && !s.labels)) return hipErrorInvalidValue;
         return s.z && (g.ldc < ((g.N + 3) & ~3) || (long)g.M * g.ldc * 4 >= (1L << 31)) ? hipErrorInvalidValue : hipSuccess;
     }
     // C (and the residual) are addressed with 32-bit byte offsets below 2 GB

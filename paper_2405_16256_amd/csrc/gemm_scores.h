@@ -3,7 +3,7 @@
 //
 // In the accumulators a lane owns one row and 32 of the wave's 64 columns, the other half wave the other 32: largest score and sum
 // of exponentials of a slot are 32 values in registers and one exchange.  The running maximum and sum of a row's softmax are put
-// together from its slots by the kernel that follows.  Bound by the 128 exponentials a thread of a 256x256 tile: 2 us beside k loops
+// together from its slots by the kernel that follows.  (Without `stats` the scores alone are written.)  Bound by the 128 exponentials a thread of a 256x256 tile: 2 us beside k loops
 // of 1.5 us a 64 values of k.
 #pragma once
 #include "gemm_tile.h"
@@ -28,7 +28,7 @@ __device__ __forceinline__ void write_scores(f32x16 (&acc)[TM][TN], int row0, in
 #pragma unroll
     for (int i = 0; i < TM; i++) {
         const int row = row0 + 32 * i + r_w;
-        label[i] = row < M ? labels[row] : -1;
+        label[i] = stats && row < M ? labels[row] : -1;
     }
     const bool ragged = col0 + SCORE_SLOT > N;
     const __amdgpu_buffer_rsrc_t rsZ = make_rsrc(z, z ? (uint32_t)((size_t)M * ldz * 4u) : 0u);
@@ -42,30 +42,32 @@ __device__ __forceinline__ void write_scores(f32x16 (&acc)[TM][TN], int row0, in
                 for (int e = 0; e < 16; e++)
                     if (col0 + 32 * j + 8 * (e >> 2) + 4 * hf + (e & 3) >= N) acc[i][j][e] = -INFINITY;
         }
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < TN; j++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) top = fmaxf(top, acc[i][j][e]);
-        top = fmaxf(top, __shfl_xor(top, 32, WAVE));
-        const float ref = top == -INFINITY ? 0.f : top;   // a slot of scores of -inf adds nothing, not NaN
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < TN; j++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - ref) * LOG2E);
-        sum += __shfl_xor(sum, 32, WAVE);
-        if (hf == 0 && row < M) stats[(size_t)slot * M + row] = make_float2(top, sum);
-        const int64_t rel = label[i] - col0;
-        const bool here = rel >= 0 && rel < SCORE_SLOT && label[i] < N;
-        if (__any(here)) {   // few slots hold the label of one of their rows
-            const int mine = here ? (int)rel - 4 * hf : -1;
-            float v = 0.f;
+        if (stats) {
+            float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < TN; j++)
 #pragma unroll
-                for (int e = 0; e < 16; e++) v = mine == 32 * j + 8 * (e >> 2) + (e & 3) ? acc[i][j][e] : v;
-            if (mine >= 0 && !(mine & 4)) picked[row] = v;   // of the two half waves the one that owns the column
+                for (int e = 0; e < 16; e++) top = fmaxf(top, acc[i][j][e]);
+            top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+            const float ref = top == -INFINITY ? 0.f : top;   // a slot of scores of -inf adds nothing, not NaN
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < TN; j++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - ref) * LOG2E);
+            sum += __shfl_xor(sum, 32, WAVE);
+            if (hf == 0 && row < M) stats[(size_t)slot * M + row] = make_float2(top, sum);
+            const int64_t rel = label[i] - col0;
+            const bool here = rel >= 0 && rel < SCORE_SLOT && label[i] < N;
+            if (__any(here)) {   // few slots hold the label of one of their rows
+                const int mine = here ? (int)rel - 4 * hf : -1;
+                float v = 0.f;
+#pragma unroll
+                for (int j = 0; j < TN; j++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) v = mine == 32 * j + 8 * (e >> 2) + (e & 3) ? acc[i][j][e] : v;
+                if (mine >= 0 && !(mine & 4)) picked[row] = v;   // of the two half waves the one that owns the column
+            }
         }
         if (z) {
             const uint32_t zrow = (uint32_t)(row0 + 32 * i + r_r);

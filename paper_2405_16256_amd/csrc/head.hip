@@ -18,6 +18,126 @@ __device__ __forceinline__ void join(float& m, float& s, float m1, float s1) {
     m = top;
 }
 
+// d = hi + lo (bf16, two rows) or d itself (fp32) of 4 columns
+__device__ __forceinline__ void put_d(bf16_t* hi_row, bf16_t* lo_row, uint32_t col, const float (&f)[4]) {
+    const uint2 hi = make_uint2(pack_bf2(f[0], f[1]), pack_bf2(f[2], f[3]));
+    *reinterpret_cast<uint2*>(hi_row + col) = hi;
+    *reinterpret_cast<uint2*>(lo_row + col) = make_uint2(pack_bf2(f[0] - lo_bf(hi.x), f[1] - hi_bf(hi.x)), pack_bf2(f[2] - lo_bf(hi.y), f[3] - hi_bf(hi.y)));
+}
+__device__ __forceinline__ void put_d(float* row, float*, uint32_t col, const float (&f)[4]) { Vec<float>::store(row + col, f); }
+// A vector of a token's row of x, zeros where it does not count (zero times NaN would be NaN in dW): for bf16 beside lo as well, so that
+// d^T x is one product over hi's rows and lo's.
+template <typename T>
+__device__ __forceinline__ void put_x(const T* __restrict__ x, T* __restrict__ xs, int row, int lo_rows, int H, int col, bool counts) {
+    typename Vec<T>::Raw v{};
+    if (counts) v = Vec<T>::raw(x + (size_t)row * H + col);
+    *reinterpret_cast<typename Vec<T>::Raw*>(xs + (size_t)row * H + col) = v;
+    if (sizeof(T) == 2) *reinterpret_cast<typename Vec<T>::Raw*>(xs + (size_t)(row + lo_rows) * H + col) = v;
+}
+
+// ------------------------------------------------------------------ whole rows
+// All scores of a row in the registers of one workgroup: read once for the largest, the sum, the loss and d.  Bound by HBM
+// (8 bytes a score in a step), by launches on small problems, of which it is one where the statistics and d apart are two, in fp32
+// three (head steps of bf16 200 tokens, hidden 512, vocabulary 2000: 26.5 -> 23.8 us; fp32 128, 256, 1000: 23.2 -> 18.6; 700,
+// 1024, 8001: 320 -> 311).  In bf16, whose statistics come with the product, it loses past 16384 columns: a workgroup of 1024 threads
+// with 32 scores each has a CU to itself, and nothing is stored while it loads (2048 rows of 32000: 104 -> 114 us).
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void k_head_row(const float* z, int ldz, const int64_t* __restrict__ labels, int N, const float* __restrict__ dloss,
+                                                      float scale, float* __restrict__ loss, T* d, int lo_rows, const T* __restrict__ x,
+                                                      T* __restrict__ xs, int H) {
+    constexpr int NW = THREADS / WAVE;
+    __shared__ float red[2 * NW];
+    const int row = (int)blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t named = labels[row];
+    const bool counts = named >= 0 && named < N;
+    const int label = counts ? (int)named : -1;
+    if (d)
+        for (int col = (int)threadIdx.x * Vec<T>::N; col < H; col += THREADS * Vec<T>::N) put_x(x, xs, row, lo_rows, H, col, counts);
+    T* const hi_row = d + (size_t)row * ldz;
+    T* const lo_row = d + (size_t)(row + lo_rows) * ldz;
+    z += (size_t)row * ldz;
+    float f[NV][4];
+    if (!counts) {
+        if (threadIdx.x == 0) loss[row] = named < 0 ? 0.f : __builtin_nanf("");
+        if (!d) return;
+#pragma unroll
+        for (int e = 0; e < 4; e++) f[0][e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const int col = 4 * (k * THREADS + (int)threadIdx.x);
+            if (col < ldz) put_d(hi_row, lo_row, (uint32_t)col, f[0]);
+        }
+        return;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < NV; k++) {
+        const int col = 4 * (k * THREADS + (int)threadIdx.x);
+#pragma unroll
+        for (int e = 0; e < 4; e++) f[k][e] = -INFINITY;
+        if (col < N) Vec<float>::load(z + (uint32_t)col, f[k]);   // rows are padded
+    }
+#pragma unroll
+    for (int k = 0; k < NV; k++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            if (4 * (k * THREADS + (int)threadIdx.x) + e >= N) f[k][e] = -INFINITY;
+            top = fmaxf(top, f[k][e]);
+        }
+    top = wave_max(top);
+    if (lane == 0) red[wave] = top;
+    __syncthreads();
+    top = red[0];
+#pragma unroll
+    for (int w = 1; w < NW; w++) top = fmaxf(top, red[w]);
+    float sum = 0.f, mine = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; k++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            if (label == 4 * (k * THREADS + (int)threadIdx.x) + e) mine = f[k][e];
+            f[k][e] = __builtin_amdgcn_exp2f((f[k][e] - top) * LOG2_E);
+            sum += f[k][e];
+        }
+    sum = wave_sum(sum);
+    if (lane == 0) red[NW + wave] = sum;
+    __syncthreads();
+    sum = red[NW];
+#pragma unroll
+    for (int w = 1; w < NW; w++) sum += red[NW + w];
+    if ((int)threadIdx.x == (label >> 2) % THREADS) loss[row] = logf(sum) + (top - mine);
+    if (!d) return;
+    const float g = dloss ? scale * dloss[row] : scale, inv = 1.f / sum;
+#pragma unroll
+    for (int k = 0; k < NV; k++) {
+        const int col = 4 * (k * THREADS + (int)threadIdx.x);
+        if (col >= ldz) continue;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const float p = f[k][e] * inv;
+            f[k][e] = col + e < N ? g * (label == col + e ? p - 1.f : p) : 0.f;
+        }
+        put_d(hi_row, lo_row, (uint32_t)col, f[k]);
+    }
+}
+
+template <typename T>
+static void launch_row(const float* z, int ldz, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss, T* d, int lo_rows,
+                       const T* x, T* xs, int H, hipStream_t st) {
+    if (ldz <= 1024) k_head_row<T, 256, 1><<<M, 256, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
+    else if (ldz <= 4096) k_head_row<T, 256, 4><<<M, 256, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
+    else if (ldz <= 8192) k_head_row<T, 512, 4><<<M, 512, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
+    else if (ldz <= 16384) k_head_row<T, 1024, 4><<<M, 1024, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
+    else if constexpr (sizeof(T) == 4) k_head_row<T, 1024, 8><<<M, 1024, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
+}
+hipError_t head_row(int dtype, const float* z, int ldz, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
+                    void* d, int lo_rows, const void* x, void* xs, int H, hipStream_t st) {
+    if (ldz > head_row_most(dtype)) return hipErrorInvalidValue;
+    if (dtype == DT_BF16) launch_row(z, ldz, labels, M, N, dloss, scale, loss, (bf16_t*)d, lo_rows, (const bf16_t*)x, (bf16_t*)xs, H, st);
+    else launch_row(z, ldz, labels, M, N, dloss, scale, loss, (float*)d, lo_rows, (const float*)x, (float*)xs, H, st);
+    return hipGetLastError();
+}
+
 // ------------------------------------------------------------------ statistics of fp32 scores
 // A workgroup reads HEAD_F32_SLOT columns of one row.  (In bf16 the product's own epilogue forms them.)
 __global__ __launch_bounds__(256) void k_head_stats(const float* __restrict__ z, int ldz, const int64_t* __restrict__ labels,
@@ -94,14 +214,11 @@ hipError_t head_rows(const float2* stats, int slots, const int64_t* labels, int 
 }
 
 // ------------------------------------------------------------------ gradient of the scores
-// A workgroup turns 1024 scores of a row into d; columns N .. ldz-1 become zeros, and so do rows that do not count, whatever their
-// scores are.  bf16: d is written as hi + lo, two bf16 numbers, lo `lo_rows` rows behind hi.  The workgroups past those of
-// the scores copy the row's x, zeros where the token does not count (zero times NaN would be NaN in dW), for bf16
-// beside lo as well: d^T x is then one product over hi's rows and lo's.
+// Of longer rows.  A workgroup turns 1024 scores of a row into d; columns N .. ldz-1 become zeros, and so do rows that do
+// not count, whatever their scores are.  The workgroups past those of the scores copy the row's x.
 template <typename T>
 __global__ __launch_bounds__(256) void k_head_grad(const float* z, int ldz, const float2* __restrict__ rows, const int64_t* __restrict__ labels,
                                                    int N, T* d, int lo_rows, const T* __restrict__ x, T* __restrict__ xs, int H, int z_wgs) {
-    constexpr bool TWO = sizeof(T) == 2;
     constexpr int PER = 1024;
     const int row = (int)blockIdx.y;
     const int64_t label = labels[row];
@@ -110,10 +227,7 @@ __global__ __launch_bounds__(256) void k_head_grad(const float* z, int ldz, cons
         constexpr int VN = Vec<T>::N;
         const int col = ((int)blockIdx.x - z_wgs) * (256 * VN) + VN * (int)threadIdx.x;
         if (col >= H) return;
-        typename Vec<T>::Raw v{};
-        if (counts) v = Vec<T>::raw(x + (size_t)row * H + col);
-        *reinterpret_cast<typename Vec<T>::Raw*>(xs + (size_t)row * H + col) = v;
-        if (TWO) *reinterpret_cast<typename Vec<T>::Raw*>(xs + (size_t)(row + lo_rows) * H + col) = v;
+        put_x(x, xs, row, lo_rows, H, col, counts);
         return;
     }
     const int col = (int)blockIdx.x * PER + 4 * (int)threadIdx.x;
@@ -128,15 +242,7 @@ __global__ __launch_bounds__(256) void k_head_grad(const float* z, int ldz, cons
             f[e] = col + e < N ? r.y * (label == col + e ? p - 1.f : p) : 0.f;
         }
     }
-    const size_t at = (size_t)row * ldz + col;
-    if constexpr (TWO) {
-        const uint2 hi = make_uint2(pack_bf2(f[0], f[1]), pack_bf2(f[2], f[3]));
-        const uint2 lo = make_uint2(pack_bf2(f[0] - lo_bf(hi.x), f[1] - hi_bf(hi.x)), pack_bf2(f[2] - lo_bf(hi.y), f[3] - hi_bf(hi.y)));
-        *reinterpret_cast<uint2*>(d + at) = hi;
-        *reinterpret_cast<uint2*>(d + at + (size_t)lo_rows * ldz) = lo;
-    } else {
-        Vec<float>::store((float*)d + at, f);   // in place of the scores
-    }
+    put_d(d + (size_t)row * ldz, d + (size_t)(row + lo_rows) * ldz, (uint32_t)col, f);
 }
 
 hipError_t head_grad(int dtype, const float* z, int ldz, const float2* rows, const int64_t* labels, int M, int N, void* d, int lo_rows,

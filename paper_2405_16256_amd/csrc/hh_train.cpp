@@ -85,6 +85,7 @@ static int head_run(hh_ctx* ctx, const HeadPlan& p, const void* x, const void* w
     float2* const stats = (float2*)at(ws, p.stats);
     float2* const rows = step ? (float2*)at(ws, p.rows) : nullptr;
     float* const z = step || !bf ? (float*)at(ws, p.z) : nullptr;
+    const bool whole = p.ld <= head_row_most(p.dt);   // a row of scores fits the registers of a workgroup
     for (int t0 = 0; t0 < p.T; t0 += p.block) {
         const int T = std::min(p.block, p.T - t0);
         for (int r0 = 0; r0 < T; r0 += p.piece) {
@@ -92,16 +93,24 @@ static int head_run(hh_ctx* ctx, const HeadPlan& p, const void* x, const void* w
             const void* const xr = at(x, (size_t)(t0 + r0) * H * es);
             const int64_t* const lab = labels + t0 + r0;
             GemmDesc g = desc(GEMM_NT, M, bf ? V : p.ld, H, xr, H, w, H, z, p.ld);
-            const GemmScores scores{z, stats, lab};
+            const GemmScores scores{z, whole && step ? nullptr : stats, lab};
             if (bf) g.scores = &scores;
             else g.b_rows = V;
             HIP_TRY(tgemm(ctx, p.dt, g, st));
+            const float* const up = dloss ? dloss + t0 + r0 : nullptr;
+            void* const d = step ? at(ws, p.d + (size_t)r0 * p.ld * es) : nullptr;
+            void* const xs = step ? at(ws, p.xs + (size_t)r0 * H * es) : nullptr;
+            if (whole && (step || !bf)) {
+                TRACED(HH_TRACE_ELEMENTWISE, (step ? 8.0 : 4.0) * M * V + (step ? (bf ? 6.0 : 8.0) * M * H : 0.0),
+                       head_row(p.dt, z, p.ld, lab, M, V, up, scale, loss + t0 + r0, d, T, xr, xs, H, st));
+                continue;
+            }
             if (!bf) TRACED(HH_TRACE_ELEMENTWISE, 4.0 * M * V, head_stats_f32(z, p.ld, lab, stats, M, V, st));
             TRACED(HH_TRACE_ELEMENTWISE, 8.0 * M * p.slots,
-                   head_rows(stats, p.slots, lab, M, V, dloss ? dloss + t0 + r0 : nullptr, scale, loss + t0 + r0, rows, st));
+                   head_rows(stats, p.slots, lab, M, V, up, scale, loss + t0 + r0, rows, st));
             if (step)
                 TRACED(HH_TRACE_ELEMENTWISE, 8.0 * M * V + (bf ? 6.0 : 8.0) * M * H,
-                       head_grad(p.dt, z, p.ld, rows, lab, M, V, at(ws, p.d + (size_t)r0 * p.ld * es), T, xr, at(ws, p.xs + (size_t)r0 * H * es), H, st));
+                       head_grad(p.dt, z, p.ld, rows, lab, M, V, d, T, xr, xs, H, st));
         }
         if (!step) continue;
         const void* const d = at(ws, p.d);

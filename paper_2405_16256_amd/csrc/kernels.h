@@ -46,7 +46,7 @@ struct GemmNorm { Each xn, r; const void* gain; float eps; };
 constexpr int NORM_K = 256;
 // An NT launch (bf16) whose result is scores [M, N] over a vocabulary of any size N: fp32 in z (rows of ldc; null: not written),
 // the largest score of a row and the sum of exp(score - largest) for each SCORE_SLOT columns in stats [slot][M], and behind
-// those, [M] floats, the score of the row's label (of a label that is no column: nothing).
+// those, [M] floats, the score of the row's label (of a label that is no column: nothing).  stats null: the scores alone.
 constexpr int SCORE_SLOT = 64;
 struct GemmScores { float* z; float2* stats; const int64_t* labels; };
 struct GemmDesc {
@@ -151,6 +151,10 @@ hipError_t attn_bwd(int dtype, const void* qkv, int ld, const void* o, const voi
 // The same of fp32 scores [M, N] in rows of ldz, slots of HEAD_F32_SLOT columns.
 constexpr int HEAD_F32_SLOT = 1024;
 hipError_t head_stats_f32(const float* z, int ldz, const int64_t* labels, float2* stats, int M, int N, hipStream_t st);
+// Whole rows of up to head_row_most() scores [M, N] at once: loss[M], and what head_grad writes where d is not null.
+constexpr int head_row_most(int dtype) { return dtype == DT_BF16 ? 16384 : 32768; }
+hipError_t head_row(int dtype, const float* z, int ldz, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
+                    void* d, int lo_rows, const void* x, void* xs, int H, hipStream_t st);
 // loss[M], and in rows[M] (null: none) the log-sum-exp of a row and the upstream gradient of its loss, 0 where it does not count
 hipError_t head_rows(const float2* stats, int slots, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
                      float2* rows, hipStream_t st);

@@ -244,4 +244,4 @@ def test_work_is_traced(ctx):
     got = hh.hh_trace_end(ctx)
     for kind in ("gemm_nt", "gemm_nn", "gemm_tn"):
         assert got[kind][0] == 1 and got[kind][2] == 2.0 * 100 * 256 * 1001
-    assert got["elementwise"][0] == 2
+    assert got["elementwise"][0] == 1
