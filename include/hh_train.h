@@ -32,8 +32,9 @@ extern "C" {
  * The scores z are never kept: the loss alone forms them in registers (HH_BF16) or for a block of tokens at a time; a step
  * holds them for a block of tokens in the workspace.
  *
- * HH_BF16: x, W, dx bfloat16; scores, statistics and losses fp32; dW fp32.  d enters the product for dx as bfloat16 and the one
- * for dW as a sum of two (16 significant bits), so that dW is an fp32 gradient and not a bfloat16 one in fp32 storage.
+ * HH_BF16: x, W, dx bfloat16; scores, statistics and losses fp32; dW fp32.  d enters the product for dx as bfloat16 (dx is rounded
+ * to that at its end anyway) and the one for dW as a sum of two, 16 significant bits: dW is within 3e-6 of the exact gradient of the
+ * given x and W (2-norm), where one bfloat16 number would leave 2e-3.
  * HH_F32: everything fp32.
  *
  * Shapes: hidden a multiple of 64 (HH_BF16) or 8 (HH_F32), at most 32768; vocab 1 .. 262144, any; tokens >= 1, any; x below 2^31
@@ -46,7 +47,7 @@ typedef struct {
 } hh_head_cfg;
 
 /* Bytes of workspace of hh_head_loss and of hh_head_step (either pointer may be NULL).  Host arithmetic only.  A step's
- * workspace grows with tokens x vocab up to a block of about 2 GiB of d. */
+ * workspace grows with tokens x vocab up to a block of 2 GiB of d beside 512 MiB of scores (HH_F32: 2 GiB of both together). */
 int hh_head_sizes(const hh_head_cfg *cfg, size_t *loss_workspace_bytes, size_t *step_workspace_bytes);
 
 /* loss[T] (fp32) of x [T, H] under the weight w [V, H] and labels[T]. */

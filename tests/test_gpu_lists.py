@@ -1,7 +1,7 @@
 """Global gradient norm with clipping and the optimizer's update over lists of tensors, against plain numbers in 64 bits.
 
 Tolerances, as relative Frobenius norms.  fp32 results: a few roundings of 2^-24 each, and the norm's one: 1e-6.  bf16
-results: one rounding of 2^-9: 2e-3 at most, 4e-3 here."""
+results: one rounding, at most 2^-8: 4e-3."""
 import math
 
 import pytest
