@@ -38,7 +38,8 @@ extern "C" {
  * HH_F32: everything fp32.
  *
  * Shapes: hidden a multiple of 64 (HH_BF16) or 8 (HH_F32), at most 32768; vocab 1 .. 262144, any; tokens >= 1, any; x below 2^31
- * bytes, W below 2^32 - 2^25 (HH_ERR_UNSUPPORTED_SHAPE otherwise).  The whole vocabulary is on this GPU. */
+ * bytes, W below 2^32 - 2^25 (HH_ERR_UNSUPPORTED_SHAPE otherwise).  The whole vocabulary is on this GPU; of a tensor-parallel share
+ * of it see hh_head_share_fwd. */
 typedef struct {
     int32_t hidden;   /* H */
     int32_t vocab;    /* V */
@@ -46,7 +47,7 @@ typedef struct {
     int32_t dtype;    /* hh_dtype */
 } hh_head_cfg;
 
-/* Bytes of workspace of hh_head_loss and of hh_head_step (either pointer may be NULL).  Host arithmetic only.  A step's
+/* Bytes of workspace of hh_head_loss, hh_head_share_fwd and of hh_head_step, hh_head_share_bwd (either pointer may be NULL).  Host arithmetic only.  A step's
  * workspace grows with tokens x vocab up to a block of 2 GiB of d beside 512 MiB of scores (HH_F32: 2 GiB of both together). */
 int hh_head_sizes(const hh_head_cfg *cfg, size_t *loss_workspace_bytes, size_t *step_workspace_bytes);
 
@@ -58,6 +59,20 @@ int hh_head_loss(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void 
 int hh_head_step(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void *w, const int64_t *labels,
                  const float *dloss, float scale, float *loss, void *dx, float *dw, int accumulate,
                  void *workspace, void *stream);
+
+/* The same under tensor parallelism, or for a vocabulary in pieces: w holds words first .. first + vocab - 1, and labels count in the
+ * whole vocabulary.  What the shares have to tell each other lies between the two calls and is not part of this library, as the
+ * all-reduces of the layers are not:
+ *     fwd:  lse[T] = log(sum over this share of exp z_tv),  picked[T] = z_t,label where the share has the label, otherwise 0
+ *     outside, over the shares:  lse = log(sum exp lse_share),  loss = lse - sum picked
+ *     bwd:  with that lse,  d_tv = g_t (exp(z_tv - lse_t) - [first + v = label(t)]);  dx is this share's partial sum, to be
+ *           added over the shares,  dW (+)= d^T x
+ * Every token with a label of 0 or more counts.  bwd forms the scores again (a third more products than hh_head_step). */
+int hh_head_share_fwd(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void *w, const int64_t *labels, int32_t first,
+                      float *lse, float *picked, void *workspace, void *stream);
+int hh_head_share_bwd(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void *w, const int64_t *labels, int32_t first,
+                      const float *lse, const float *dloss, float scale, void *dx, float *dw, int accumulate,
+                      void *workspace, void *stream);
 
 /* Global gradient norm and clipping over n tensors of any sizes:
  *     norm = sqrt(sum of all g^2),  factor = min(1, max_norm / (norm + 1e-6)),  out = factor * g

@@ -32,7 +32,7 @@ WEIGHT_FIELDS = ("g_attn", "wq", "wk", "wv", "wo", "g_mlp", "w_gate", "w_up", "w
 EXPORTS = ("hh_last_error", "hh_ctx_create", "hh_ctx_destroy", "hh_ctx_reserve", "hh_layer_flops", "hh_layer_sizes",
            "hh_saved_layout_of", "hh_layer_fwd", "hh_layer_fwd_noalloc", "hh_layer_bwd", "hh_stage_sizes", "hh_stage_step", "hh_stage_step_1f1b", "hh_layer_profile", "hh_trace_begin",
            "hh_trace_end", "hh_sim_pipeline", "hh_sim_weighted_mean", "hh_plan_layers", "hh_plan_order", "hh_plan_cluster",
-           "hh_head_sizes", "hh_head_loss", "hh_head_step", "hh_grad_clip", "hh_adamw_step")
+           "hh_head_sizes", "hh_head_loss", "hh_head_step", "hh_head_share_fwd", "hh_head_share_bwd", "hh_grad_clip", "hh_adamw_step")
 TRACE_KINDS = ("gemm_nt", "gemm_nn", "gemm_tn", "attn_fwd", "attn_bwd", "elementwise")
 
 
@@ -153,6 +153,8 @@ def _load() -> C.CDLL:
         "hh_head_sizes": [C.POINTER(hh_head_cfg), sz, sz],
         "hh_head_loss": [vp, C.POINTER(hh_head_cfg), vp, vp, vp, vp, vp, vp],
         "hh_head_step": [vp, C.POINTER(hh_head_cfg), vp, vp, vp, vp, C.c_float, vp, vp, vp, i, vp, vp],
+        "hh_head_share_fwd": [vp, C.POINTER(hh_head_cfg), vp, vp, vp, C.c_int32, vp, vp, vp, vp],
+        "hh_head_share_bwd": [vp, C.POINTER(hh_head_cfg), vp, vp, vp, C.c_int32, vp, vp, C.c_float, vp, vp, i, vp, vp],
         "hh_grad_clip": [vp, i, C.POINTER(hh_clip_tensor), C.c_float, vp, vp, vp],
         "hh_adamw_step": [vp, C.POINTER(hh_adamw_cfg), i, C.POINTER(hh_adamw_tensor), vp, vp],
     }
@@ -379,6 +381,17 @@ def hh_head_step(ctx, cfg: hh_head_cfg, x, w, labels, dloss, scale, loss, dx, dw
     """dloss: fp32 upstream gradients of the tokens' losses (times scale), or None for scale alone."""
     _check(lib.hh_head_step(ctx, C.byref(cfg), _ptr(x), _ptr(w), _ptr(labels), _ptr(dloss), float(scale), _ptr(loss), _ptr(dx), _ptr(dw),
                             int(accumulate), _ptr(workspace), stream))
+
+
+def hh_head_share_fwd(ctx, cfg: hh_head_cfg, x, w, labels, first, lse, picked, workspace, stream=0) -> None:
+    """w: words first .. first + cfg.vocab - 1 of the vocabulary that the labels count in."""
+    _check(lib.hh_head_share_fwd(ctx, C.byref(cfg), _ptr(x), _ptr(w), _ptr(labels), int(first), _ptr(lse), _ptr(picked), _ptr(workspace), stream))
+
+
+def hh_head_share_bwd(ctx, cfg: hh_head_cfg, x, w, labels, first, lse, dloss, scale, dx, dw, accumulate, workspace, stream=0) -> None:
+    """lse: of the whole vocabulary; dx: this share's partial sum."""
+    _check(lib.hh_head_share_bwd(ctx, C.byref(cfg), _ptr(x), _ptr(w), _ptr(labels), int(first), _ptr(lse), _ptr(dloss), float(scale), _ptr(dx),
+                                 _ptr(dw), int(accumulate), _ptr(workspace), stream))
 
 
 _DTYPES = {torch.float32: HH_F32, torch.bfloat16: HH_BF16}

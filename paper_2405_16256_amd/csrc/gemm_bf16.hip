@@ -92,7 +92,8 @@ __device__ __forceinline__ void place_loop() {
 }
 
 // NT or NN; RES: a problem has a residual, which is added to C.  A kernel of its own: what it holds costs the others registers.
-// SCORES: the one problem (NT) ends in write_scores: C is z, R the labels, `partial` the statistics, and no tile is cut.
+// SCORES: the one problem (NT) ends in write_scores: C is z, R the labels, `accumulate` the first word, `partial` the statistics, and no
+// tile is cut.
 template <int KIND, bool RES, bool SCORES = false>
 __global__ __launch_bounds__(512) void k_gemm_dma(DmaGroup grp, int full, int n_items, float* __restrict__ partial) {
     // The workgroup walks work items blockIdx.x, + gridDim.x, ... < n_items.  Items below `full` are whole tiles
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(512) void k_gemm_dma(DmaGroup grp, int full, int n_
 
         if constexpr (SCORES) {
             const DmaProblem& g = grp.p[0];
-            write_scores(acc, cm0 + wm, cn0 + wn, g.M, g.N, (float*)g.C, g.ldc, (const int64_t*)g.R, (float2*)partial,
+            write_scores(acc, cm0 + wm, cn0 + wn, g.M, g.N, (float*)g.C, g.ldc, (const int64_t*)g.R, g.accumulate, (float2*)partial,
                          smem + DSTAGES * 2 * DSTAGE_BYTES + wave * 4096);
             if (!has_next) return;
             continue;
@@ -691,6 +692,7 @@ static hipError_t launch_dma(const GemmDesc* g, int n, hipStream_t st) {
     if constexpr (SCORES) {
         grp.p[0].C = g[0].scores->z;
         grp.p[0].R = (const bf16_t*)g[0].scores->labels;
+        grp.p[0].accumulate = g[0].scores->first;
         grp.ksplit = divisor(1);
         kern<<<tiles < NUM_CU ? tiles : NUM_CU, 512, LDS, st>>>(grp, tiles, tiles, (float*)g[0].scores->stats);
         return hipGetLastError();
@@ -1265,6 +1267,7 @@ static hipError_t launch_ring_scores(const GemmDesc& g, hipStream_t st) {
     p.A.p[0] = const_cast<void*>(g.A); p.B.p[0] = const_cast<void*>(g.B); p.C.p[0] = g.scores->z;
     p.R.p[0] = const_cast<int64_t*>(g.scores->labels);
     p.partial = (float*)g.scores->stats;
+    p.accumulate = g.scores->first;
     p.kseg[0] = p.kseg[1] = INT_MAX;
     p.a_bytes = (uint32_t)extent_a(g); p.b_bytes = (uint32_t)extent_b(g, g.K);
     p.lda = g.lda; p.ldb = g.ldb; p.ldc = g.ldc; p.M = g.M; p.N = g.N; p.K = g.K;

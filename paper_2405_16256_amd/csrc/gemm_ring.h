@@ -81,7 +81,7 @@ __device__ __forceinline__ float rotated(float v) { return __int_as_float(__buil
 // LDS for all of k; only B goes through the ring.  Bound by latency: the launch before it (3.6 us with the gap behind it, of rows of 256)
 // goes, and the workgroups get 1.2 to 1.9 us longer, for about 500 instructions between x and its place in LDS and because what waits for
 // x and the gain, which the compiler counts, waits for the requests of B behind them too.
-// SCORES: the tile ends in write_scores: C is z, R the labels, `partial` the statistics.
+// SCORES: the tile ends in write_scores: C is z, R the labels, `accumulate` the first word, `partial` the statistics.
 template <int KIND, int MB, bool F, int BM, int BN, int WM, int WN, int NS, bool NORM = false, bool SCORES = false>
 __device__ __forceinline__ void ring_body(const RingProblem<MB, F>& g, const RingNorm<MB>* norm = nullptr, bool writer = false) {
     if constexpr (NORM) asm volatile("" ::"s"(norm->gain), "s"(norm->eps), "s"(g.K), "s"(g.M), "s"(g.N));
@@ -512,7 +512,7 @@ __device__ __forceinline__ void ring_body(const RingProblem<MB, F>& g, const Rin
 
     if constexpr (SCORES) {
         __syncthreads();   // nobody reads the ring any more
-        write_scores(acc, m0 + wm, n0 + wn, M, N, (float*)Cv, ldc, (const int64_t*)R, (float2*)g.partial, smem + wave * 4096);
+        write_scores(acc, m0 + wm, n0 + wn, M, N, (float*)Cv, ldc, (const int64_t*)R, g.accumulate, (float2*)g.partial, smem + wave * 4096);
         return;
     }
 

@@ -12,10 +12,10 @@
 namespace hh {
 
 // rows row0 + 32 i + lane % 32, columns col0 + 32 j + 8 q + 4 (lane / 32) + e of [M, N]; z: null or rows of ldz >= N rounded up to 4.
-// patch: 4 KB of LDS that this wave alone uses.
+// Column c is word first + c of the vocabulary that the labels count in.  patch: 4 KB of LDS that this wave alone uses.
 template <int TM, int TN>
 __device__ __forceinline__ void write_scores(f32x16 (&acc)[TM][TN], int row0, int col0, int M, int N, float* z, int ldz,
-                                             const int64_t* __restrict__ labels, float2* __restrict__ stats, char* patch) {
+                                             const int64_t* __restrict__ labels, int first, float2* __restrict__ stats, char* patch) {
     static_assert(32 * TN == SCORE_SLOT, "a wave owns whole slots");
     constexpr float LOG2E = 1.4426950408889634f;
     if (col0 >= N) return;   // no column of the slot is there
@@ -28,7 +28,7 @@ __device__ __forceinline__ void write_scores(f32x16 (&acc)[TM][TN], int row0, in
 #pragma unroll
     for (int i = 0; i < TM; i++) {
         const int row = row0 + 32 * i + r_w;
-        label[i] = stats && row < M ? labels[row] : -1;
+        label[i] = stats && row < M ? labels[row] : (int64_t)first - 1;
     }
     const bool ragged = col0 + SCORE_SLOT > N;
     const __amdgpu_buffer_rsrc_t rsZ = make_rsrc(z, z ? (uint32_t)((size_t)M * ldz * 4u) : 0u);
@@ -57,8 +57,8 @@ __device__ __forceinline__ void write_scores(f32x16 (&acc)[TM][TN], int row0, in
                 for (int e = 0; e < 16; e++) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - ref) * LOG2E);
             sum += __shfl_xor(sum, 32, WAVE);
             if (hf == 0 && row < M) stats[(size_t)slot * M + row] = make_float2(top, sum);
-            const int64_t rel = label[i] - col0;
-            const bool here = rel >= 0 && rel < SCORE_SLOT && label[i] < N;
+            const int64_t rel = label[i] - first - col0;
+            const bool here = rel >= 0 && rel < SCORE_SLOT && col0 + rel < N;
             if (__any(here)) {   // few slots hold the label of one of their rows
                 const int mine = here ? (int)rel - 4 * hf : -1;
                 float v = 0.f;

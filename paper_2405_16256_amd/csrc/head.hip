@@ -42,13 +42,13 @@ __device__ __forceinline__ void put_x(const T* __restrict__ x, T* __restrict__ x
 // 1024, 8001: 320 -> 311).  In bf16, whose statistics come with the product, it loses past 16384 columns: a workgroup of 1024 threads
 // with 32 scores each has a CU to itself, and nothing is stored while it loads (2048 rows of 32000: 104 -> 114 us).
 template <typename T, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS) void k_head_row(const float* z, int ldz, const int64_t* __restrict__ labels, int N, const float* __restrict__ dloss,
-                                                      float scale, float* __restrict__ loss, T* d, int lo_rows, const T* __restrict__ x,
-                                                      T* __restrict__ xs, int H) {
+__global__ __launch_bounds__(THREADS) void k_head_row(HeadTokens t, const float* z, int ldz, float* __restrict__ loss, T* d, int lo_rows,
+                                                      const T* __restrict__ x, T* __restrict__ xs, int H) {
+    const int N = t.N;
     constexpr int NW = THREADS / WAVE;
     __shared__ float red[2 * NW];
     const int row = (int)blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t named = labels[row];
+    const int64_t named = t.labels[row];
     const bool counts = named >= 0 && named < N;
     const int label = counts ? (int)named : -1;
     if (d)
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(THREADS) void k_head_row(const float* z, int ldz, c
     for (int w = 1; w < NW; w++) sum += red[NW + w];
     if ((int)threadIdx.x == (label >> 2) % THREADS) loss[row] = logf(sum) + (top - mine);
     if (!d) return;
-    const float g = dloss ? scale * dloss[row] : scale, inv = 1.f / sum;
+    const float g = t.dloss ? t.scale * t.dloss[row] : t.scale, inv = 1.f / sum;
 #pragma unroll
     for (int k = 0; k < NV; k++) {
         const int col = 4 * (k * THREADS + (int)threadIdx.x);
@@ -122,26 +122,25 @@ __global__ __launch_bounds__(THREADS) void k_head_row(const float* z, int ldz, c
 }
 
 template <typename T>
-static void launch_row(const float* z, int ldz, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss, T* d, int lo_rows,
-                       const T* x, T* xs, int H, hipStream_t st) {
-    if (ldz <= 1024) k_head_row<T, 256, 1><<<M, 256, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
-    else if (ldz <= 4096) k_head_row<T, 256, 4><<<M, 256, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
-    else if (ldz <= 8192) k_head_row<T, 512, 4><<<M, 512, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
-    else if (ldz <= 16384) k_head_row<T, 1024, 4><<<M, 1024, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
-    else if constexpr (sizeof(T) == 4) k_head_row<T, 1024, 8><<<M, 1024, 0, st>>>(z, ldz, labels, N, dloss, scale, loss, d, lo_rows, x, xs, H);
+static void launch_row(const HeadTokens& t, const float* z, int ldz, float* loss, T* d, int lo_rows, const T* x, T* xs, int H, hipStream_t st) {
+    if (ldz <= 1024) k_head_row<T, 256, 1><<<t.M, 256, 0, st>>>(t, z, ldz, loss, d, lo_rows, x, xs, H);
+    else if (ldz <= 4096) k_head_row<T, 256, 4><<<t.M, 256, 0, st>>>(t, z, ldz, loss, d, lo_rows, x, xs, H);
+    else if (ldz <= 8192) k_head_row<T, 512, 4><<<t.M, 512, 0, st>>>(t, z, ldz, loss, d, lo_rows, x, xs, H);
+    else if (ldz <= 16384) k_head_row<T, 1024, 4><<<t.M, 1024, 0, st>>>(t, z, ldz, loss, d, lo_rows, x, xs, H);
+    else if constexpr (sizeof(T) == 4) k_head_row<T, 1024, 8><<<t.M, 1024, 0, st>>>(t, z, ldz, loss, d, lo_rows, x, xs, H);
 }
-hipError_t head_row(int dtype, const float* z, int ldz, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
-                    void* d, int lo_rows, const void* x, void* xs, int H, hipStream_t st) {
-    if (ldz > head_row_most(dtype)) return hipErrorInvalidValue;
-    if (dtype == DT_BF16) launch_row(z, ldz, labels, M, N, dloss, scale, loss, (bf16_t*)d, lo_rows, (const bf16_t*)x, (bf16_t*)xs, H, st);
-    else launch_row(z, ldz, labels, M, N, dloss, scale, loss, (float*)d, lo_rows, (const float*)x, (float*)xs, H, st);
+hipError_t head_row(int dtype, const HeadTokens& t, const float* z, int ldz, float* loss, void* d, int lo_rows, const void* x, void* xs, int H,
+                    hipStream_t st) {
+    if (ldz > head_row_most(dtype) || t.first || t.limit != t.N) return hipErrorInvalidValue;
+    if (dtype == DT_BF16) launch_row(t, z, ldz, loss, (bf16_t*)d, lo_rows, (const bf16_t*)x, (bf16_t*)xs, H, st);
+    else launch_row(t, z, ldz, loss, (float*)d, lo_rows, (const float*)x, (float*)xs, H, st);
     return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ statistics of fp32 scores
 // A workgroup reads HEAD_F32_SLOT columns of one row.  (In bf16 the product's own epilogue forms them.)
-__global__ __launch_bounds__(256) void k_head_stats(const float* __restrict__ z, int ldz, const int64_t* __restrict__ labels,
-                                                    float2* __restrict__ stats, int M, int N) {
+__global__ __launch_bounds__(256) void k_head_stats(HeadTokens t, const float* __restrict__ z, int ldz, float2* __restrict__ stats) {
+    const int M = t.M, N = t.N;
     const int row = (int)blockIdx.y, slot = (int)blockIdx.x, col = slot * HEAD_F32_SLOT + 4 * (int)threadIdx.x;
     float f[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if (col < N) {
@@ -150,7 +149,7 @@ __global__ __launch_bounds__(256) void k_head_stats(const float* __restrict__ z,
         for (int e = 0; e < 4; e++)
             if (col + e >= N) f[e] = -INFINITY;
     }
-    const int64_t label = labels[row];
+    const int64_t label = t.labels[row] - t.first;
     if (label >= col && label < col + 4 && label < N)
         ((float*)(stats + (size_t)gridDim.x * M))[row] = label == col ? f[0] : label == col + 1 ? f[1] : label == col + 2 ? f[2] : f[3];
     __shared__ float red[8];
@@ -166,8 +165,8 @@ __global__ __launch_bounds__(256) void k_head_stats(const float* __restrict__ z,
     if (threadIdx.x == 0) stats[(size_t)slot * M + row] = make_float2(top, sum);
 }
 
-hipError_t head_stats_f32(const float* z, int ldz, const int64_t* labels, float2* stats, int M, int N, hipStream_t st) {
-    k_head_stats<<<dim3((N + HEAD_F32_SLOT - 1) / HEAD_F32_SLOT, M), 256, 0, st>>>(z, ldz, labels, stats, M, N);
+hipError_t head_stats_f32(const HeadTokens& t, const float* z, int ldz, float2* stats, hipStream_t st) {
+    k_head_stats<<<dim3((t.N + HEAD_F32_SLOT - 1) / HEAD_F32_SLOT, t.M), 256, 0, st>>>(t, z, ldz, stats);
     return hipGetLastError();
 }
 
@@ -175,8 +174,9 @@ hipError_t head_stats_f32(const float* z, int ldz, const int64_t* labels, float2
 // 4 rows a workgroup, 64 threads a row: the rows' statistics of a slot are 32 bytes, and there are workgroups for every CU from 1024
 // tokens on (16 rows of 64 threads: 700 tokens, 782 slots 8.9 us, 333 tokens, 1563 slots 13.8).
 constexpr int ROWS_WG = 4;
-__global__ __launch_bounds__(256) void k_head_rows(const float2* __restrict__ stats, int slots, const int64_t* __restrict__ labels, int M, int N,
-                                                   const float* __restrict__ dloss, float scale, float* __restrict__ loss, float2* __restrict__ rows) {
+__global__ __launch_bounds__(256) void k_head_rows(HeadTokens t, const float2* __restrict__ stats, int slots, float* __restrict__ loss,
+                                                   float* __restrict__ lse_out, float* __restrict__ picked_out) {
+    const int M = t.M;
     __shared__ float2 part[4][ROWS_WG];
     const int r = threadIdx.x & (ROWS_WG - 1), row = (int)blockIdx.x * ROWS_WG + r, from = threadIdx.x / ROWS_WG;
     float m = -INFINITY, s = 0.f;
@@ -199,17 +199,15 @@ __global__ __launch_bounds__(256) void k_head_rows(const float2* __restrict__ st
 #pragma unroll
     for (int w = 1; w < 4; w++) join(m, s, part[w][r].x, part[w][r].y);
     const float lse = m + logf(s);
-    const int64_t label = labels[row];
-    const bool counts = label >= 0 && label < N;
-    const float* const picked = (const float*)(stats + (size_t)slots * M);
-    loss[row] = counts ? lse - picked[row] : label < 0 ? 0.f : __builtin_nanf("");
-    // the column of the one-hot vector, -1 where the token does not count, beside what k_head_grad multiplies by
-    if (rows) rows[row] = make_float2(lse, counts ? (dloss ? scale * dloss[row] : scale) : 0.f);
+    const int64_t label = t.labels[row], column = label - t.first;
+    const float picked = column >= 0 && column < t.N ? ((const float*)(stats + (size_t)slots * M))[row] : 0.f;
+    if (loss) loss[row] = label < 0 ? 0.f : label < t.limit ? lse - picked : __builtin_nanf("");
+    if (lse_out) lse_out[row] = lse;
+    if (picked_out) picked_out[row] = label < 0 ? 0.f : picked;
 }
 
-hipError_t head_rows(const float2* stats, int slots, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
-                     float2* rows, hipStream_t st) {
-    k_head_rows<<<(M + ROWS_WG - 1) / ROWS_WG, 256, 0, st>>>(stats, slots, labels, M, N, dloss, scale, loss, rows);
+hipError_t head_rows(const HeadTokens& t, const float2* stats, int slots, float* loss, float* lse, float* picked, hipStream_t st) {
+    k_head_rows<<<(t.M + ROWS_WG - 1) / ROWS_WG, 256, 0, st>>>(t, stats, slots, loss, lse, picked);
     return hipGetLastError();
 }
 
@@ -217,41 +215,41 @@ hipError_t head_rows(const float2* stats, int slots, const int64_t* labels, int 
 // Of longer rows.  A workgroup turns 1024 scores of a row into d; columns N .. ldz-1 become zeros, and so do rows that do
 // not count, whatever their scores are.  The workgroups past those of the scores copy the row's x.
 template <typename T>
-__global__ __launch_bounds__(256) void k_head_grad(const float* z, int ldz, const float2* __restrict__ rows, const int64_t* __restrict__ labels,
-                                                   int N, T* d, int lo_rows, const T* __restrict__ x, T* __restrict__ xs, int H, int z_wgs) {
+__global__ __launch_bounds__(256) void k_head_grad(HeadTokens t, const float* z, int ldz, const float* __restrict__ lse, T* d, int lo_rows,
+                                                   const T* __restrict__ x, T* __restrict__ xs, int H, int z_wgs) {
     constexpr int PER = 1024;
     const int row = (int)blockIdx.y;
-    const int64_t label = labels[row];
-    const bool counts = label >= 0 && label < N;
+    const int64_t label = t.labels[row];
+    const bool counts = label >= 0 && label < t.limit;
     if ((int)blockIdx.x >= z_wgs) {
         constexpr int VN = Vec<T>::N;
         const int col = ((int)blockIdx.x - z_wgs) * (256 * VN) + VN * (int)threadIdx.x;
-        if (col >= H) return;
-        put_x(x, xs, row, lo_rows, H, col, counts);
+        if (col < H) put_x(x, xs, row, lo_rows, H, col, counts);
         return;
     }
     const int col = (int)blockIdx.x * PER + 4 * (int)threadIdx.x;
     if (col >= ldz) return;
     float f[4] = {0.f, 0.f, 0.f, 0.f};
-    if (counts && col < N) {
-        const float2 r = rows[row];
+    if (counts && col < t.N) {
+        const float ref = lse[row], g = t.dloss ? t.scale * t.dloss[row] : t.scale;
+        const int64_t column = label - t.first;
         Vec<float>::load(z + (size_t)row * ldz + col, f);
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            const float p = __builtin_amdgcn_exp2f((f[e] - r.x) * LOG2_E);
-            f[e] = col + e < N ? r.y * (label == col + e ? p - 1.f : p) : 0.f;
+            const float p = __builtin_amdgcn_exp2f((f[e] - ref) * LOG2_E);
+            f[e] = col + e < t.N ? g * (column == col + e ? p - 1.f : p) : 0.f;
         }
     }
     put_d(d + (size_t)row * ldz, d + (size_t)(row + lo_rows) * ldz, (uint32_t)col, f);
 }
 
-hipError_t head_grad(int dtype, const float* z, int ldz, const float2* rows, const int64_t* labels, int M, int N, void* d, int lo_rows,
-                     const void* x, void* xs, int H, hipStream_t st) {
+hipError_t head_grad(int dtype, const HeadTokens& t, const float* z, int ldz, const float* lse, void* d, int lo_rows, const void* x, void* xs, int H,
+                     hipStream_t st) {
     const int z_wgs = (ldz + 1023) / 1024;
     if (dtype == DT_BF16)
-        k_head_grad<bf16_t><<<dim3(z_wgs + (H + 2047) / 2048, M), 256, 0, st>>>(z, ldz, rows, labels, N, (bf16_t*)d, lo_rows, (const bf16_t*)x, (bf16_t*)xs, H, z_wgs);
+        k_head_grad<bf16_t><<<dim3(z_wgs + (H + 2047) / 2048, t.M), 256, 0, st>>>(t, z, ldz, lse, (bf16_t*)d, lo_rows, (const bf16_t*)x, (bf16_t*)xs, H, z_wgs);
     else
-        k_head_grad<float><<<dim3(z_wgs + (H + 1023) / 1024, M), 256, 0, st>>>(z, ldz, rows, labels, N, (float*)d, lo_rows, (const float*)x, (float*)xs, H, z_wgs);
+        k_head_grad<float><<<dim3(z_wgs + (H + 1023) / 1024, t.M), 256, 0, st>>>(t, z, ldz, lse, (float*)d, lo_rows, (const float*)x, (float*)xs, H, z_wgs);
     return hipGetLastError();
 }
 

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdint>
 
 #include "ctx.h"
 #include "kernels.h"
@@ -29,10 +30,12 @@ static int check_head(const hh_head_cfg* c) {
 struct HeadPlan {
     int dt, T, H, V, ld, slots;   // ld: a row of scores and of d
     int block, piece;             // tokens
-    size_t stats, rows, z, d, xs, gemm_ws, total;
+    bool whole;                   // a row of scores fits the registers of a workgroup
+    size_t stats, lse, z, d, xs, gemm_ws, total;
 };
 static int split_evenly(int n, int most) { const int parts = (n + most - 1) / most; return (n + parts - 1) / parts; }
-static HeadPlan head_plan(const hh_head_cfg* c, bool step) {
+// share: of a vocabulary that other devices have the rest of.
+static HeadPlan head_plan(const hh_head_cfg* c, bool step, bool share) {
     HeadPlan p{};
     const bool bf = c->dtype == HH_BF16;
     p.dt = bf ? DT_BF16 : DT_F32;
@@ -44,14 +47,15 @@ static HeadPlan head_plan(const hh_head_cfg* c, bool step) {
     const long most = std::min<long>(std::min<long>(((1L << 31) - 1) / (4L * p.ld), ((1L << 31) - 1) / (4L * p.H)), 32768);
     p.block = split_evenly(p.T, (int)std::max<long>(most, 1));
     p.piece = p.block;
-    if (bf && step) {
-        const long rows = std::max<long>(256, (1L << 29) / (4L * p.ld) / 256 * 256);
-        p.piece = (int)std::min<long>(p.block, rows);
+    p.whole = p.ld <= head_row_most(p.dt) && (step || !bf) && !share;
+    if (bf) {   // up to 512 MB of scores (a step of 4096 x 32000 in pieces of 256 MB: 10.77 -> 10.58 ms), 256 MB of statistics
+        const long rows = step ? (1L << 29) / (4L * p.ld) : (1L << 28) / (8L * p.slots);
+        p.piece = (int)std::min<long>(p.block, std::max<long>(256, rows / 256 * 256));
     }
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += up256(bytes); return o; };
-    p.stats = take((size_t)p.slots * p.piece * sizeof(float2) + (size_t)p.piece * sizeof(float));
-    if (step) p.rows = take((size_t)p.piece * sizeof(float2));
+    if (!p.whole) p.stats = take((size_t)p.slots * p.piece * sizeof(float2) + (size_t)p.piece * sizeof(float));
+    if (step && !p.whole) p.lse = take((size_t)p.piece * sizeof(float));
     if (step || !bf) p.z = take((size_t)p.piece * p.ld * 4);
     if (step) {
         p.d = bf ? take((size_t)p.block * p.ld * 4) : p.z;
@@ -64,8 +68,8 @@ static HeadPlan head_plan(const hh_head_cfg* c, bool step) {
 
 extern "C" int hh_head_sizes(const hh_head_cfg* cfg, size_t* loss_workspace_bytes, size_t* step_workspace_bytes) {
     TRY(check_head(cfg));
-    if (loss_workspace_bytes) *loss_workspace_bytes = head_plan(cfg, false).total;
-    if (step_workspace_bytes) *step_workspace_bytes = head_plan(cfg, true).total;
+    if (loss_workspace_bytes) *loss_workspace_bytes = std::max(head_plan(cfg, false, false).total, head_plan(cfg, false, true).total);
+    if (step_workspace_bytes) *step_workspace_bytes = std::max(head_plan(cfg, true, false).total, head_plan(cfg, true, true).total);
     return HH_OK;
 }
 
@@ -75,49 +79,61 @@ extern "C" int hh_head_sizes(const hh_head_cfg* cfg, size_t* loss_workspace_byte
         HIP_TRY(call);                                    \
     } while (0)
 
-static int head_run(hh_ctx* ctx, const HeadPlan& p, const void* x, const void* w, const int64_t* labels, const float* dloss, float scale,
-                    float* loss, void* dx, float* dw, int accumulate, void* ws, hipStream_t st) {
-    const bool bf = p.dt == DT_BF16, step = dx != nullptr;
+// What a call is given and asked for, by token: of a step dx and dw; lse_in: the log-sum-exp over a vocabulary of which w is a share.
+struct HeadCall {
+    const void *x, *w;
+    const int64_t* labels;
+    int64_t first, limit;
+    const float* dloss;
+    float scale;
+    float *loss, *lse, *picked;
+    const float* lse_in;
+    void* dx;
+    float* dw;
+    int accumulate;
+};
+static int head_run(hh_ctx* ctx, const HeadPlan& p, const HeadCall& c, void* ws, hipStream_t st) {
+    const bool bf = p.dt == DT_BF16, step = c.dx != nullptr;
     const size_t es = dt_size(p.dt);
     const int H = p.H, V = p.V;
     ctx->gemm_ws = step ? at(ws, p.gemm_ws) : nullptr;
     ctx->gemm_room = 0;
-    float2* const stats = (float2*)at(ws, p.stats);
-    float2* const rows = step ? (float2*)at(ws, p.rows) : nullptr;
+    float2* const stats = p.whole || c.lse_in ? nullptr : (float2*)at(ws, p.stats);
     float* const z = step || !bf ? (float*)at(ws, p.z) : nullptr;
-    const bool whole = p.ld <= head_row_most(p.dt);   // a row of scores fits the registers of a workgroup
     for (int t0 = 0; t0 < p.T; t0 += p.block) {
         const int T = std::min(p.block, p.T - t0);
         for (int r0 = 0; r0 < T; r0 += p.piece) {
-            const int M = std::min(p.piece, T - r0);
-            const void* const xr = at(x, (size_t)(t0 + r0) * H * es);
-            const int64_t* const lab = labels + t0 + r0;
-            GemmDesc g = desc(GEMM_NT, M, bf ? V : p.ld, H, xr, H, w, H, z, p.ld);
-            const GemmScores scores{z, whole && step ? nullptr : stats, lab};
+            const int M = std::min(p.piece, T - r0), at0 = t0 + r0;
+            const void* const xr = at(c.x, (size_t)at0 * H * es);
+            const HeadTokens t{c.labels + at0, c.first, c.limit, M, V, c.dloss ? c.dloss + at0 : nullptr, c.scale};
+            auto from = [&](float* q) { return q ? q + at0 : nullptr; };
+            GemmDesc g = desc(GEMM_NT, M, bf ? V : p.ld, H, xr, H, c.w, H, z, p.ld);
+            const GemmScores scores{z, stats, t.labels, (int)c.first};
             if (bf) g.scores = &scores;
             else g.b_rows = V;
             HIP_TRY(tgemm(ctx, p.dt, g, st));
-            const float* const up = dloss ? dloss + t0 + r0 : nullptr;
             void* const d = step ? at(ws, p.d + (size_t)r0 * p.ld * es) : nullptr;
             void* const xs = step ? at(ws, p.xs + (size_t)r0 * H * es) : nullptr;
-            if (whole && (step || !bf)) {
-                TRACED(HH_TRACE_ELEMENTWISE, (step ? 8.0 : 4.0) * M * V + (step ? (bf ? 6.0 : 8.0) * M * H : 0.0),
-                       head_row(p.dt, z, p.ld, lab, M, V, up, scale, loss + t0 + r0, d, T, xr, xs, H, st));
+            const double grad_bytes = 8.0 * M * V + (bf ? 6.0 : 8.0) * M * H;
+            if (p.whole) {
+                TRACED(HH_TRACE_ELEMENTWISE, step ? grad_bytes : 4.0 * M * V, head_row(p.dt, t, z, p.ld, from(c.loss), d, T, xr, xs, H, st));
                 continue;
             }
-            if (!bf) TRACED(HH_TRACE_ELEMENTWISE, 4.0 * M * V, head_stats_f32(z, p.ld, lab, stats, M, V, st));
-            TRACED(HH_TRACE_ELEMENTWISE, 8.0 * M * p.slots,
-                   head_rows(stats, p.slots, lab, M, V, up, scale, loss + t0 + r0, rows, st));
-            if (step)
-                TRACED(HH_TRACE_ELEMENTWISE, 8.0 * M * V + (bf ? 6.0 : 8.0) * M * H,
-                       head_grad(p.dt, z, p.ld, rows, lab, M, V, d, T, xr, xs, H, st));
+            const float* lse = c.lse_in ? c.lse_in + at0 : nullptr;
+            if (!lse) {
+                float* const out = step ? (float*)at(ws, p.lse) : from(c.lse);
+                if (!bf) TRACED(HH_TRACE_ELEMENTWISE, 4.0 * M * V, head_stats_f32(t, z, p.ld, stats, st));
+                TRACED(HH_TRACE_ELEMENTWISE, 8.0 * M * p.slots, head_rows(t, stats, p.slots, from(c.loss), out, from(c.picked), st));
+                lse = out;
+            }
+            if (step) TRACED(HH_TRACE_ELEMENTWISE, grad_bytes, head_grad(p.dt, t, z, p.ld, lse, d, T, xr, xs, H, st));
         }
         if (!step) continue;
         const void* const d = at(ws, p.d);
         const void* const xs = at(ws, p.xs);
         GemmDesc g[4];
         int n = 0;
-        g[n] = desc(GEMM_NN, T, H, p.ld, d, p.ld, w, H, at(dx, (size_t)t0 * H * es), H);
+        g[n] = desc(GEMM_NN, T, H, p.ld, d, p.ld, c.w, H, at(c.dx, (size_t)t0 * H * es), H);
         g[n++].b_rows = V;
         if (!bf && gemm_f32_long_k_better(T, H, p.ld)) {
             g[0].long_k = 1;
@@ -128,8 +144,8 @@ static int head_run(hh_ctx* ctx, const HeadPlan& p, const void* x, const void* w
         const int most = (int)std::min<long>(V, std::max<long>(256, ((1L << 31) - 1) / (4L * H) / 256 * 256));
         for (int v0 = 0; v0 < V; v0 += most) {
             if (n == 4) { HIP_TRY(tgemm(ctx, p.dt, g, n, st)); n = 0; }
-            g[n++] = desc(GEMM_TN, std::min(most, V - v0), H, bf ? 2 * T : T, at(d, (size_t)v0 * es), p.ld, xs, H, dw + (size_t)v0 * H, H,
-                          nullptr, 0, 1, accumulate || t0 > 0);
+            g[n++] = desc(GEMM_TN, std::min(most, V - v0), H, bf ? 2 * T : T, at(d, (size_t)v0 * es), p.ld, xs, H, c.dw + (size_t)v0 * H, H,
+                          nullptr, 0, 1, c.accumulate || t0 > 0);
             g[n - 1].pair = bf;
         }
         HIP_TRY(tgemm(ctx, p.dt, g, n, st));
@@ -143,17 +159,55 @@ extern "C" int hh_head_loss(hh_ctx* ctx, const hh_head_cfg* cfg, const void* x, 
     TRY(check_ptr(x, "x")); TRY(check_ptr(w, "w")); TRY(check_ptr(labels, "labels")); TRY(check_ptr(loss, "loss"));
     TRY(check_ptr(workspace, "workspace"));
     if (!ctx) return fail(HH_ERR_INVALID_ARG, "ctx is NULL");
-    return head_run(ctx, head_plan(cfg, false), x, w, labels, nullptr, 0.f, loss, nullptr, nullptr, 0, workspace, (hipStream_t)stream);
+    HeadCall c{};
+    c.x = x; c.w = w; c.labels = labels; c.limit = cfg->vocab; c.loss = loss;
+    return head_run(ctx, head_plan(cfg, false, false), c, workspace, (hipStream_t)stream);
+}
+
+static int check_dloss(const float* dloss) {
+    return (uintptr_t)dloss & 15 ? fail(HH_ERR_MISALIGNED, "dloss is not 16-byte aligned") : (int)HH_OK;
 }
 
 extern "C" int hh_head_step(hh_ctx* ctx, const hh_head_cfg* cfg, const void* x, const void* w, const int64_t* labels, const float* dloss,
                             float scale, float* loss, void* dx, float* dw, int accumulate, void* workspace, void* stream) {
     TRY(check_head(cfg));
     TRY(check_ptr(x, "x")); TRY(check_ptr(w, "w")); TRY(check_ptr(labels, "labels")); TRY(check_ptr(loss, "loss"));
-    TRY(check_ptr(dx, "dx")); TRY(check_ptr(dw, "dw")); TRY(check_ptr(workspace, "workspace"));
-    if ((uintptr_t)dloss & 15) return fail(HH_ERR_MISALIGNED, "dloss is not 16-byte aligned");
+    TRY(check_ptr(dx, "dx")); TRY(check_ptr(dw, "dw")); TRY(check_ptr(workspace, "workspace")); TRY(check_dloss(dloss));
     if (!ctx) return fail(HH_ERR_INVALID_ARG, "ctx is NULL");
-    return head_run(ctx, head_plan(cfg, true), x, w, labels, dloss, scale, loss, dx, dw, accumulate, workspace, (hipStream_t)stream);
+    HeadCall c{};
+    c.x = x; c.w = w; c.labels = labels; c.limit = cfg->vocab; c.dloss = dloss; c.scale = scale;
+    c.loss = loss; c.dx = dx; c.dw = dw; c.accumulate = accumulate;
+    return head_run(ctx, head_plan(cfg, true, false), c, workspace, (hipStream_t)stream);
+}
+
+static int check_share(const hh_head_cfg* cfg, int32_t first) {
+    TRY(check_head(cfg));
+    if (first < 0 || first > INT32_MAX - cfg->vocab) return fail(HH_ERR_INVALID_ARG, "first (%d) is negative, or the share ends past 2^31 - 1", first);
+    return HH_OK;
+}
+
+extern "C" int hh_head_share_fwd(hh_ctx* ctx, const hh_head_cfg* cfg, const void* x, const void* w, const int64_t* labels, int32_t first,
+                                 float* lse, float* picked, void* workspace, void* stream) {
+    TRY(check_share(cfg, first));
+    TRY(check_ptr(x, "x")); TRY(check_ptr(w, "w")); TRY(check_ptr(labels, "labels")); TRY(check_ptr(lse, "lse"));
+    TRY(check_ptr(picked, "picked")); TRY(check_ptr(workspace, "workspace"));
+    if (!ctx) return fail(HH_ERR_INVALID_ARG, "ctx is NULL");
+    HeadCall c{};
+    c.x = x; c.w = w; c.labels = labels; c.first = first; c.limit = INT64_MAX; c.lse = lse; c.picked = picked;
+    return head_run(ctx, head_plan(cfg, false, true), c, workspace, (hipStream_t)stream);
+}
+
+extern "C" int hh_head_share_bwd(hh_ctx* ctx, const hh_head_cfg* cfg, const void* x, const void* w, const int64_t* labels, int32_t first,
+                                 const float* lse, const float* dloss, float scale, void* dx, float* dw, int accumulate,
+                                 void* workspace, void* stream) {
+    TRY(check_share(cfg, first));
+    TRY(check_ptr(x, "x")); TRY(check_ptr(w, "w")); TRY(check_ptr(labels, "labels")); TRY(check_ptr(lse, "lse"));
+    TRY(check_ptr(dx, "dx")); TRY(check_ptr(dw, "dw")); TRY(check_ptr(workspace, "workspace")); TRY(check_dloss(dloss));
+    if (!ctx) return fail(HH_ERR_INVALID_ARG, "ctx is NULL");
+    HeadCall c{};
+    c.x = x; c.w = w; c.labels = labels; c.first = first; c.limit = INT64_MAX; c.dloss = dloss; c.scale = scale;
+    c.lse_in = lse; c.dx = dx; c.dw = dw; c.accumulate = accumulate;
+    return head_run(ctx, head_plan(cfg, true, true), c, workspace, (hipStream_t)stream);
 }
 
 // ------------------------------------------------------------------ lists of tensors

@@ -48,7 +48,8 @@ constexpr int NORM_K = 256;
 // the largest score of a row and the sum of exp(score - largest) for each SCORE_SLOT columns in stats [slot][M], and behind
 // those, [M] floats, the score of the row's label (of a label that is no column: nothing).  stats null: the scores alone.
 constexpr int SCORE_SLOT = 64;
-struct GemmScores { float* z; float2* stats; const int64_t* labels; };
+// Column c is word first + c of the vocabulary that the labels count in.
+struct GemmScores { float* z; float2* stats; const int64_t* labels; int first; };
 struct GemmDesc {
     int kind;
     int M, N, K;
@@ -148,20 +149,24 @@ hipError_t attn_bwd(int dtype, const void* qkv, int ld, const void* o, const voi
 
 // ---- output projection and softmax cross entropy (head.hip).  stats: [slot][M] (largest score, sum of exponentials) and behind them
 // [M] floats, the labels' scores, as of GemmScores.
+// What the calls below share: M tokens; the columns are words first .. first + N - 1, and a token counts whose label is from 0 to
+// limit - 1.
+struct HeadTokens { const int64_t* labels; int64_t first, limit; int M, N; const float* dloss; float scale; };
 // The same of fp32 scores [M, N] in rows of ldz, slots of HEAD_F32_SLOT columns.
 constexpr int HEAD_F32_SLOT = 1024;
-hipError_t head_stats_f32(const float* z, int ldz, const int64_t* labels, float2* stats, int M, int N, hipStream_t st);
-// Whole rows of up to head_row_most() scores [M, N] at once: loss[M], and what head_grad writes where d is not null.
+hipError_t head_stats_f32(const HeadTokens& t, const float* z, int ldz, float2* stats, hipStream_t st);
+// Whole rows of up to head_row_most() scores, of a whole vocabulary, at once: loss[M], and what head_grad writes where d is not null.
 constexpr int head_row_most(int dtype) { return dtype == DT_BF16 ? 16384 : 32768; }
-hipError_t head_row(int dtype, const float* z, int ldz, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
-                    void* d, int lo_rows, const void* x, void* xs, int H, hipStream_t st);
-// loss[M], and in rows[M] (null: none) the log-sum-exp of a row and the upstream gradient of its loss, 0 where it does not count
-hipError_t head_rows(const float2* stats, int slots, const int64_t* labels, int M, int N, const float* dloss, float scale, float* loss,
-                     float2* rows, hipStream_t st);
-// d from the scores z (rows of ldz both, the padding zeros), in bf16 as two matrices, the second lo_rows rows behind the first, in
-// fp32 in place; and x [M, H] with zeros for the tokens that do not count, in bf16 a second time lo_rows rows behind.
-hipError_t head_grad(int dtype, const float* z, int ldz, const float2* rows, const int64_t* labels, int M, int N, void* d, int lo_rows,
-                     const void* x, void* xs, int H, hipStream_t st);
+hipError_t head_row(int dtype, const HeadTokens& t, const float* z, int ldz, float* loss, void* d, int lo_rows, const void* x, void* xs, int H,
+                    hipStream_t st);
+// From the statistics of a row, each where it is not null: loss[M], lse[M] its log-sum-exp, picked[M] its label's score, 0 where that
+// is no column.
+hipError_t head_rows(const HeadTokens& t, const float2* stats, int slots, float* loss, float* lse, float* picked, hipStream_t st);
+// d from the scores z (rows of ldz both, the padding zeros) and the log-sum-exp of their rows, in bf16 as two matrices, the second lo_rows
+// rows behind the first, in fp32 in place; and x [M, H] with zeros for the tokens that do not count, in bf16 a second time lo_rows
+// rows behind.
+hipError_t head_grad(int dtype, const HeadTokens& t, const float* z, int ldz, const float* lse, void* d, int lo_rows, const void* x, void* xs, int H,
+                     hipStream_t st);
 
 // ---- lists of tensors (tensors.hip)
 constexpr int CLIP_CHUNK = 8192, ADAMW_CHUNK = 2048;   // elements that a workgroup takes at a time

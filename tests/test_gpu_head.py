@@ -189,6 +189,46 @@ def test_pieces_of_the_vocabulary(ctx):
     check("bf16", step(ctx, "bf16", x, w, labels, scale=1.0 / tokens), ref)
 
 
+# shares of one word, of no whole slot, that begin and end inside slots and tiles; past 32768 words; none but one share
+@pytest.mark.parametrize("kind,hidden,tokens,cuts", [("bf16", 64, 70, [0, 1, 64, 130]), ("bf16", 512, 300, [0, 2500, 5003]), ("bf16", 256, 129, [0, 300, 40001]),
+                                                     ("bf16", 1024, 700, [0, 12500, 25000, 37500, 50001]), ("f32", 40, 33, [0, 7, 8, 1200]),
+                                                     ("f32", 256, 128, [0, 1000]), ("f32", 64, 50, [0, 33000, 40001])])
+def test_shares_of_the_vocabulary(ctx, kind, hidden, tokens, cuts):
+    """Each share by itself; the sums over the shares are those of the whole vocabulary.  dx: a share's partial sum is rounded once, so
+    the total is off by as much of the partial sums as each of them may be."""
+    vocab = cuts[-1]
+    x, w, labels = inputs(kind, hidden, vocab, tokens)
+    labels[::7] = torch.tensor([cuts[1 % (len(cuts) - 1)], vocab - 1, 0], device=DEV).repeat(tokens)[:len(labels[::7])]   # the shares' first and last words
+    x[labels < 0] = float("nan")
+    dloss = torch.rand(tokens, device=DEV)
+    loss, dx, dw = definition(torch.nan_to_num(x), w, labels, 0.5 * dloss)
+    found, lse = [], torch.full((tokens,), float("-inf"), device=DEV, dtype=torch.float64)
+    for a, b in zip(cuts, cuts[1:]):
+        cfg = hh.make_head_cfg(hidden, b - a, tokens, hh.HH_BF16 if kind == "bf16" else hh.HH_F32)
+        sizes = hh.hh_head_sizes(cfg)
+        s, picked = (torch.full((tokens,), 7.0, device=DEV) for _ in range(2))
+        share = w[a:b].clone()
+        hh.hh_head_share_fwd(ctx, cfg, x, share, labels, a, s, picked, torch.full((sizes[0],), 255, dtype=torch.uint8, device=DEV), stream())
+        here = (labels >= a) & (labels < b)
+        assert (picked[~here] == 0).all()
+        lse = torch.where(labels >= 0, torch.logaddexp(lse, s.double()), torch.zeros_like(lse))
+        found.append((cfg, sizes, share, a, b, picked))
+    total = torch.where(labels >= 0, lse - sum(f[5].double() for f in found), torch.zeros_like(lse))
+    assert off(total, loss) <= FP32
+    lse = lse.float()
+    lse[labels < 0] = float("nan")           # what does not count is not looked at
+    got, partial = torch.zeros(tokens, hidden, device=DEV, dtype=torch.float64), 0.0
+    for cfg, sizes, share, a, b, _ in found:
+        dxs, before = torch.full_like(x, 7.0), torch.randn(b - a, hidden, device=DEV) * 0.01
+        dws = before.clone()
+        hh.hh_head_share_bwd(ctx, cfg, x, share, labels, a, lse, dloss, 0.5, dxs, dws, True, torch.full((sizes[1],), 255, dtype=torch.uint8, device=DEV), stream())
+        assert off(dws, dw[a:b] + before.double()) <= FP32
+        assert (dxs[labels < 0] == 0).all()
+        got += dxs.double()
+        partial += float(torch.linalg.vector_norm(dxs.double()))
+    assert float(torch.linalg.vector_norm(got - dx)) <= (BF16 if kind == "bf16" else FP32) * partial
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_differences(ctx, kind):
     """Both gradients against differences of the loss itself, taken in 64 bits along random directions."""

@@ -1,12 +1,32 @@
 """hh_train.h: host-side sizes, and refusals before any GPU work.  Runs without a GPU."""
 import ctypes as C
+import os
+import subprocess
 
 import pytest
 import torch
 
 from paper_2405_16256_amd import binding as hh
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 A, ODD = 1 << 20, (1 << 20) + 2          # addresses: aligned, aligned to two bytes
+
+
+def test_structs_are_those_of_the_header(tmp_path):
+    """The header is C, and the binding's structs have its fields' places."""
+    structs = {n: getattr(hh, n) for n in ("hh_head_cfg", "hh_clip_tensor", "hh_adamw_tensor", "hh_adamw_cfg")}
+    lines = ["#include <stdio.h>", '#include "hh_train.h"', "int main(void) {"]
+    for n, s in structs.items():
+        lines.append('printf("%s %%zu", sizeof(%s));' % (n, n))
+        lines += ['printf(" %%zu", offsetof(%s, %s));' % (n, f) for f, _ in s._fields_] + ['printf("\\n");']
+    lines += ['printf("clip %zu\\n", HH_CLIP_WORKSPACE_BYTES); return 0; }']
+    src, exe = tmp_path / "s.c", tmp_path / "s"
+    src.write_text("\n".join(lines))
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    out = dict(line.split(" ", 1) for line in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines())
+    for n, s in structs.items():
+        assert [int(t) for t in out[n].split()] == [C.sizeof(s)] + [getattr(s, f).offset for f, _ in s._fields_], n
+    assert int(out["clip"]) == hh.HH_CLIP_WORKSPACE_BYTES
 
 
 def head(**kw):
@@ -23,7 +43,7 @@ def test_head_sizes():
     # the workspace of a step is bounded however many tokens there are, and d never reaches 2^31 bytes
     assert hh.hh_head_sizes(head(tokens=200000))[1] < 3 << 30
     assert hh.hh_head_sizes(head(vocab=262144, hidden=64, tokens=1 << 20))[1] < 3 << 30
-    assert hh.hh_head_sizes(head(dtype=hh.HH_F32))[0] > 4 * 2048 * 32000
+    assert hh.hh_head_sizes(head(dtype=hh.HH_F32))[0] >= 4 * 2048 * 32000
     loss_only = C.c_size_t()
     assert hh.lib.hh_head_sizes(C.byref(head()), C.byref(loss_only), None) == hh.HH_OK and loss_only.value == loss
 
@@ -62,6 +82,27 @@ def test_head_refuses_pointers():
             assert name in str(e.value) or (name == "dloss" and p is None and "ctx" in str(e.value))   # dloss may be missing
     assert hh.lib.hh_head_loss(None, None, A, A, A, A, A, None) == hh.HH_ERR_INVALID_ARG
     assert hh.lib.hh_head_sizes(None, None, None) == hh.HH_ERR_INVALID_ARG
+
+
+def test_shares_refuse():
+    cfg = head()
+    for call, good in ((hh.hh_head_share_fwd, dict(x=A, w=A, labels=A, lse=A, picked=A, workspace=A)),
+                       (hh.hh_head_share_bwd, dict(x=A, w=A, labels=A, lse=A, dloss=None, scale=1.0, dx=A, dw=A, accumulate=0, workspace=A))):
+        for name in good:
+            if name in ("scale", "accumulate"):
+                continue
+            for p, code in ((None, hh.HH_ERR_INVALID_ARG), (ODD, hh.HH_ERR_MISALIGNED)):
+                with pytest.raises(hh.HHError) as e:
+                    call(None, cfg, first=0, **{**good, name: p})
+                assert e.value.code == code
+                assert name in str(e.value) or (name == "dloss" and p is None and "ctx" in str(e.value))
+        for first in (-1, 2 ** 31 - 32000):
+            with pytest.raises(hh.HHError) as e:
+                call(None, cfg, first=first, **good)
+            assert e.value.code == hh.HH_ERR_INVALID_ARG and "first" in str(e.value)
+        with pytest.raises(hh.HHError) as e:
+            call(None, head(hidden=100), first=0, **good)
+        assert e.value.code == hh.HH_ERR_UNSUPPORTED_SHAPE
 
 
 def clip_list(**kw):
