@@ -845,7 +845,7 @@ static constexpr Variant VARIANTS[V_COUNT] = {
 };
 static constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8};
 // The input gradient of an output projection has k loops of hundreds of stages over a vocabulary and few tiles: more splits to choose
-// from.  700x1024x50048: 8 shares of 24 tiles 115 us, 10 shares 105; 333x4096x32000: 4 shares of 48 tiles 114, 5 shares 112.
+// from.  700x1024x50048: 8 shares of 24 tiles 119 us, 10 shares 105; 333x4096x32000: 4 shares of 48 tiles 119, 5 shares 112.
 static constexpr int VOCAB_SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24};
 struct Splits { const int *from, *to; const int* begin() const { return from; } const int* end() const { return to; } };
 static Splits splits_of(const GemmDesc& g) { return g.b_rows ? Splits{std::begin(VOCAB_SPLITS), std::end(VOCAB_SPLITS)} : Splits{std::begin(SPLITS), std::end(SPLITS)}; }

@@ -3,8 +3,8 @@
 //
 // In the accumulators a lane owns one row and 32 of the wave's 64 columns, the other half wave the other 32: largest score and sum
 // of exponentials of a slot are 32 values in registers and one exchange.  The running maximum and sum of a row's softmax are put
-// together from its slots by the kernel that follows.  (Without `stats` the scores alone are written.)  Bound by the 128 exponentials a thread of a 256x256 tile: 2 us beside k loops
-// of 1.5 us a 64 values of k.
+// together from its slots by the kernel that follows.  Without `stats` the scores alone are written.  Bound by the k loop:
+// 2048x32000x4096 425 us without z (1.26 PFLOP/s), 465 with its 262 MB.
 #pragma once
 #include "gemm_tile.h"
 #include "kernels.h"
