@@ -47,8 +47,9 @@ typedef struct {
     int32_t dtype;    /* hh_dtype */
 } hh_head_cfg;
 
-/* Bytes of workspace of hh_head_loss, hh_head_share_fwd and of hh_head_step, hh_head_share_bwd (either pointer may be NULL).  Host arithmetic only.  A step's
- * workspace grows with tokens x vocab up to a block of 2 GiB of d beside 512 MiB of scores (HH_F32: 2 GiB of both together). */
+/* Bytes of workspace of hh_head_loss, hh_head_share_fwd and of hh_head_step, hh_head_share_bwd (either pointer may be NULL).
+ * Host arithmetic only.  A step's workspace grows with tokens x vocab up to a block of 2 GiB of d beside 512 MiB of scores
+ * (HH_F32: 2 GiB of both together). */
 int hh_head_sizes(const hh_head_cfg *cfg, size_t *loss_workspace_bytes, size_t *step_workspace_bytes);
 
 /* loss[T] (fp32) of x [T, H] under the weight w [V, H] and labels[T]. */
@@ -94,8 +95,8 @@ int hh_grad_clip(hh_ctx *ctx, int n, const hh_clip_tensor *tensors, float max_no
 /* One step of Adam with decoupled weight decay on n tensors:
  *     g' = factor * g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
  *     p = p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + decay p)
- * in fp32, with constants formed in fp64.  factor: device, fp32, one value (result + 1 of hh_grad_clip: clipped gradients need not be written and read
- * again), or NULL for 1; a factor that is not finite leaves every tensor as it is.  A bfloat16 parameter has an fp32 master
+ * in fp32, with constants formed in fp64.  factor: device, fp32, one value (result + 1 of hh_grad_clip: clipped gradients need
+ * not be written and read again), or NULL for 1; a factor that is not finite leaves every tensor as it is.  A bfloat16 parameter has an fp32 master
  * copy, which is p above, and receives p rounded; an fp32 parameter is its own master copy (master NULL).  step counts from 1.
  * Pointers, tensors, n and counts as in hh_grad_clip. */
 typedef struct {

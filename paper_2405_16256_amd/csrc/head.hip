@@ -212,8 +212,9 @@ hipError_t head_rows(const HeadTokens& t, const float2* stats, int slots, float*
 }
 
 // ------------------------------------------------------------------ gradient of the scores
-// Of longer rows.  Bound by HBM: 2048 rows of 32000 91 us, 5.9 TB/s of scores in and d out.  A workgroup turns 1024 scores of a row into d; columns N .. ldz-1 become zeros, and so do rows that do
-// not count, whatever their scores are.  The workgroups past those of the scores copy the row's x.
+// Of longer rows.  Bound by HBM: 2048 rows of 32000 91 us, 5.9 TB/s of scores in and d out.  A workgroup turns 1024 scores of a
+// row into d; columns N .. ldz-1 become zeros, and so do rows that do not count, whatever their scores are.  The workgroups past
+// those of the scores copy the row's x.
 template <typename T>
 __global__ __launch_bounds__(256) void k_head_grad(HeadTokens t, const float* z, int ldz, const float* __restrict__ lse, T* d, int lo_rows,
                                                    const T* __restrict__ x, T* __restrict__ xs, int H, int z_wgs) {

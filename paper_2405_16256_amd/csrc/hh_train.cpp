@@ -356,7 +356,8 @@ extern "C" int hh_adamw_step(hh_ctx* ctx, const hh_adamw_cfg* cfg, int n, const 
     if (!ctx) return fail(HH_ERR_INVALID_ARG, "ctx is NULL");
     const hipStream_t st = (hipStream_t)stream;
     const double bc1 = 1.0 - std::pow(cfg->beta1, (double)cfg->step), bc2 = 1.0 - std::pow(cfg->beta2, (double)cfg->step);
-    const AdamwHyper h{(float)cfg->beta1, (float)(1.0 - cfg->beta1), (float)cfg->beta2, (float)(1.0 - cfg->beta2), (float)cfg->eps, (float)(cfg->lr / bc1), (float)(1.0 / std::sqrt(bc2))};
+    const AdamwHyper h{(float)cfg->beta1, (float)(1.0 - cfg->beta1), (float)cfg->beta2, (float)(1.0 - cfg->beta2), (float)cfg->eps,
+                       (float)(cfg->lr / bc1), (float)(1.0 / std::sqrt(bc2))};
     auto fill = [&](const hh_adamw_tensor& q, AdamwItem& t) { fill_adamw(q, cfg->lr, t); };
     Traced t_(ctx, st, HH_TRACE_ELEMENTWISE, 1, bytes);
     return for_lists<AdamwList, ADAMW_LIST, ADAMW_CHUNK>(n, tensors, fill, [&](const AdamwList& l) -> int {
