@@ -68,7 +68,9 @@ int hh_head_step(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void 
  *     outside, over the shares:  lse = log(sum exp lse_share),  loss = lse - sum picked
  *     bwd:  with that lse,  d_tv = g_t (exp(z_tv - lse_t) - [first + v = label(t)]);  dx is this share's partial sum, to be
  *           added over the shares,  dW (+)= d^T x
- * Every token with a label of 0 or more counts.  bwd forms the scores again (a third more products than hh_head_step). */
+ * Every token with a label of 0 or more counts.  bwd forms the scores again (a third more products than hh_head_step).  lse is one fp32
+ * number, rounded in each share and again outside: that moves a loss by up to 2^-23 |lse| and exp(z - lse) by as much of itself, where
+ * hh_head_step keeps the largest score and the sum apart and loses nothing to large scores. */
 int hh_head_share_fwd(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void *w, const int64_t *labels, int32_t first,
                       float *lse, float *picked, void *workspace, void *stream);
 int hh_head_share_bwd(hh_ctx *ctx, const hh_head_cfg *cfg, const void *x, const void *w, const int64_t *labels, int32_t first,

@@ -2,8 +2,10 @@
 // gradient.
 //
 // Row t of z has the statistics (largest score, sum of exponentials) of each slot of its columns.  k_head_rows puts them together,
-//     m = max_s m_s,  lse = m + log(sum_s S_s exp(m_s - m)),
-// and k_head_grad reads the scores once and writes d_tv = g_t (exp(z_tv - lse_t) - [v = label(t)]).  All of it in fp32.
+//     m = max_s m_s,  S = sum_s S_s exp(m_s - m),  loss = log S + (m - z_t,label),
+// and k_head_grad reads the scores once and writes d_tv = g_t (exp(z_tv - m) / S - [v = label(t)]).  All of it in fp32.  m and S stay
+// two numbers: their one, m + log S, has the ulp of a score, which would be the relative error of all of a row's p and the
+// absolute one of its loss (scores around 1000: 3e-5).  Shares of a vocabulary, which have only that one from outside, are off by it.
 #include "common.h"
 #include "kernels.h"
 
@@ -175,7 +177,7 @@ hipError_t head_stats_f32(const HeadTokens& t, const float* z, int ldz, float2* 
 // tokens on.  Bound by latency: 700 tokens, 782 slots 5.9 us (8.9 with 16 rows of 64 threads), 333 tokens, 1563 slots 7.0 (13.8).
 constexpr int ROWS_WG = 4;
 __global__ __launch_bounds__(256) void k_head_rows(HeadTokens t, const float2* __restrict__ stats, int slots, float* __restrict__ loss,
-                                                   float* __restrict__ lse_out, float* __restrict__ picked_out) {
+                                                   float* __restrict__ lse_out, float2* __restrict__ norm_out, float* __restrict__ picked_out) {
     const int M = t.M;
     __shared__ float2 part[4][ROWS_WG];
     const int r = threadIdx.x & (ROWS_WG - 1), row = (int)blockIdx.x * ROWS_WG + r, from = threadIdx.x / ROWS_WG;
@@ -198,26 +200,27 @@ __global__ __launch_bounds__(256) void k_head_rows(HeadTokens t, const float2* _
     m = part[0][r].x; s = part[0][r].y;
 #pragma unroll
     for (int w = 1; w < 4; w++) join(m, s, part[w][r].x, part[w][r].y);
-    const float lse = m + logf(s);
+    const float log_s = logf(s);
     const int64_t label = t.labels[row], column = label - t.first;
     const float picked = column >= 0 && column < t.N ? ((const float*)(stats + (size_t)slots * M))[row] : 0.f;
-    if (loss) loss[row] = label < 0 ? 0.f : label < t.limit ? lse - picked : __builtin_nanf("");
-    if (lse_out) lse_out[row] = lse;
+    if (loss) loss[row] = label < 0 ? 0.f : label < t.limit ? log_s + (m - picked) : __builtin_nanf("");
+    if (lse_out) lse_out[row] = m + log_s;
+    if (norm_out) norm_out[row] = make_float2(m, 1.f / s);
     if (picked_out) picked_out[row] = label < 0 ? 0.f : picked;
 }
 
-hipError_t head_rows(const HeadTokens& t, const float2* stats, int slots, float* loss, float* lse, float* picked, hipStream_t st) {
-    k_head_rows<<<(t.M + ROWS_WG - 1) / ROWS_WG, 256, 0, st>>>(t, stats, slots, loss, lse, picked);
+hipError_t head_rows(const HeadTokens& t, const float2* stats, int slots, float* loss, float* lse, float2* norm, float* picked, hipStream_t st) {
+    k_head_rows<<<(t.M + ROWS_WG - 1) / ROWS_WG, 256, 0, st>>>(t, stats, slots, loss, lse, norm, picked);
     return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ gradient of the scores
 // Of longer rows.  Bound by HBM: 2048 rows of 32000 91 us, 5.9 TB/s of scores in and d out.  A workgroup turns 1024 scores of a
 // row into d; columns N .. ldz-1 become zeros, and so do rows that do not count, whatever their scores are.  The workgroups past
-// those of the scores copy the row's x.
+// those of the scores copy the row's x.  p = exp(z - m) / S from norm, exp(z - lse) where that is null.
 template <typename T>
-__global__ __launch_bounds__(256) void k_head_grad(HeadTokens t, const float* z, int ldz, const float* __restrict__ lse, T* d, int lo_rows,
-                                                   const T* __restrict__ x, T* __restrict__ xs, int H, int z_wgs) {
+__global__ __launch_bounds__(256) void k_head_grad(HeadTokens t, const float* z, int ldz, const float2* __restrict__ norm, const float* __restrict__ lse,
+                                                   T* d, int lo_rows, const T* __restrict__ x, T* __restrict__ xs, int H, int z_wgs) {
     constexpr int PER = 1024;
     const int row = (int)blockIdx.y;
     const int64_t label = t.labels[row];
@@ -232,25 +235,28 @@ __global__ __launch_bounds__(256) void k_head_grad(HeadTokens t, const float* z,
     if (col >= ldz) return;
     float f[4] = {0.f, 0.f, 0.f, 0.f};
     if (counts && col < t.N) {
-        const float ref = lse[row], g = t.dloss ? t.scale * t.dloss[row] : t.scale;
+        const float2 of = norm ? norm[row] : make_float2(lse[row], 1.f);
+        const float g = t.dloss ? t.scale * t.dloss[row] : t.scale;
         const int64_t column = label - t.first;
         Vec<float>::load(z + (size_t)row * ldz + col, f);
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            const float p = __builtin_amdgcn_exp2f((f[e] - ref) * LOG2_E);
+            const float p = __builtin_amdgcn_exp2f((f[e] - of.x) * LOG2_E) * of.y;
             f[e] = col + e < t.N ? g * (column == col + e ? p - 1.f : p) : 0.f;
         }
     }
     put_d(d + (size_t)row * ldz, d + (size_t)(row + lo_rows) * ldz, (uint32_t)col, f);
 }
 
-hipError_t head_grad(int dtype, const HeadTokens& t, const float* z, int ldz, const float* lse, void* d, int lo_rows, const void* x, void* xs, int H,
-                     hipStream_t st) {
+hipError_t head_grad(int dtype, const HeadTokens& t, const float* z, int ldz, const float2* norm, const float* lse, void* d, int lo_rows, const void* x,
+                     void* xs, int H, hipStream_t st) {
     const int z_wgs = (ldz + 1023) / 1024;
     if (dtype == DT_BF16)
-        k_head_grad<bf16_t><<<dim3(z_wgs + (H + 2047) / 2048, t.M), 256, 0, st>>>(t, z, ldz, lse, (bf16_t*)d, lo_rows, (const bf16_t*)x, (bf16_t*)xs, H, z_wgs);
+        k_head_grad<bf16_t><<<dim3(z_wgs + (H + 2047) / 2048, t.M), 256, 0, st>>>(t, z, ldz, norm, lse, (bf16_t*)d, lo_rows, (const bf16_t*)x,
+                                                                                         (bf16_t*)xs, H, z_wgs);
     else
-        k_head_grad<float><<<dim3(z_wgs + (H + 1023) / 1024, t.M), 256, 0, st>>>(t, z, ldz, lse, (float*)d, lo_rows, (const float*)x, (float*)xs, H, z_wgs);
+        k_head_grad<float><<<dim3(z_wgs + (H + 1023) / 1024, t.M), 256, 0, st>>>(t, z, ldz, norm, lse, (float*)d, lo_rows, (const float*)x, (float*)xs, H,
+                                                                                        z_wgs);
     return hipGetLastError();
 }
 

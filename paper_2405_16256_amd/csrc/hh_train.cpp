@@ -31,7 +31,7 @@ struct HeadPlan {
     int dt, T, H, V, ld, slots;   // ld: a row of scores and of d
     int block, piece;             // tokens
     bool whole;                   // a row of scores fits the registers of a workgroup
-    size_t stats, lse, z, d, xs, gemm_ws, total;
+    size_t stats, norm, z, d, xs, gemm_ws, total;
 };
 static int split_evenly(int n, int most) { const int parts = (n + most - 1) / most; return (n + parts - 1) / parts; }
 // share: of a vocabulary that other devices have the rest of.
@@ -55,7 +55,7 @@ static HeadPlan head_plan(const hh_head_cfg* c, bool step, bool share) {
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += up256(bytes); return o; };
     if (!p.whole) p.stats = take((size_t)p.slots * p.piece * sizeof(float2) + (size_t)p.piece * sizeof(float));
-    if (step && !p.whole) p.lse = take((size_t)p.piece * sizeof(float));
+    if (step && !p.whole && !share) p.norm = take((size_t)p.piece * sizeof(float2));
     if (step || !bf) p.z = take((size_t)p.piece * p.ld * 4);
     if (step) {
         p.d = bf ? take((size_t)p.block * p.ld * 4) : p.z;
@@ -119,14 +119,13 @@ static int head_run(hh_ctx* ctx, const HeadPlan& p, const HeadCall& c, void* ws,
                 TRACED(HH_TRACE_ELEMENTWISE, step ? grad_bytes : 4.0 * M * V, head_row(p.dt, t, z, p.ld, from(c.loss), d, T, xr, xs, H, st));
                 continue;
             }
-            const float* lse = c.lse_in ? c.lse_in + at0 : nullptr;
+            const float* const lse = c.lse_in ? c.lse_in + at0 : nullptr;
+            float2* const norm = step && !lse ? (float2*)at(ws, p.norm) : nullptr;
             if (!lse) {
-                float* const out = step ? (float*)at(ws, p.lse) : from(c.lse);
                 if (!bf) TRACED(HH_TRACE_ELEMENTWISE, 4.0 * M * V, head_stats_f32(t, z, p.ld, stats, st));
-                TRACED(HH_TRACE_ELEMENTWISE, 8.0 * M * p.slots, head_rows(t, stats, p.slots, from(c.loss), out, from(c.picked), st));
-                lse = out;
+                TRACED(HH_TRACE_ELEMENTWISE, 8.0 * M * p.slots, head_rows(t, stats, p.slots, from(c.loss), from(c.lse), norm, from(c.picked), st));
             }
-            if (step) TRACED(HH_TRACE_ELEMENTWISE, grad_bytes, head_grad(p.dt, t, z, p.ld, lse, d, T, xr, xs, H, st));
+            if (step) TRACED(HH_TRACE_ELEMENTWISE, grad_bytes, head_grad(p.dt, t, z, p.ld, norm, lse, d, T, xr, xs, H, st));
         }
         if (!step) continue;
         const void* const d = at(ws, p.d);

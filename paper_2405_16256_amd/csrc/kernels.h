@@ -159,14 +159,14 @@ hipError_t head_stats_f32(const HeadTokens& t, const float* z, int ldz, float2* 
 constexpr int head_row_most(int dtype) { return dtype == DT_BF16 ? 16384 : 32768; }
 hipError_t head_row(int dtype, const HeadTokens& t, const float* z, int ldz, float* loss, void* d, int lo_rows, const void* x, void* xs, int H,
                     hipStream_t st);
-// From the statistics of a row, each where it is not null: loss[M], lse[M] its log-sum-exp, picked[M] its label's score, 0 where that
-// is no column.
-hipError_t head_rows(const HeadTokens& t, const float2* stats, int slots, float* loss, float* lse, float* picked, hipStream_t st);
-// d from the scores z (rows of ldz both, the padding zeros) and the log-sum-exp of their rows, in bf16 as two matrices, the second lo_rows
-// rows behind the first, in fp32 in place; and x [M, H] with zeros for the tokens that do not count, in bf16 a second time lo_rows
-// rows behind.
-hipError_t head_grad(int dtype, const HeadTokens& t, const float* z, int ldz, const float* lse, void* d, int lo_rows, const void* x, void* xs, int H,
-                     hipStream_t st);
+// From the statistics of a row, each where it is not null: loss[M], lse[M] its log-sum-exp, norm[M] its largest score and one over its sum
+// of exponentials, picked[M] its label's score, 0 where that is no column.
+hipError_t head_rows(const HeadTokens& t, const float2* stats, int slots, float* loss, float* lse, float2* norm, float* picked, hipStream_t st);
+// d from the scores z (rows of ldz both, the padding zeros) and their rows' norm, or log-sum-exp where norm is null, in bf16 as two
+// matrices, the second lo_rows rows behind the first, in fp32 in place; and x [M, H] with zeros for the tokens that do not count, in
+// bf16 a second time lo_rows rows behind.
+hipError_t head_grad(int dtype, const HeadTokens& t, const float* z, int ldz, const float2* norm, const float* lse, void* d, int lo_rows, const void* x,
+                     void* xs, int H, hipStream_t st);
 
 // ---- lists of tensors (tensors.hip)
 constexpr int CLIP_CHUNK = 8192, ADAMW_CHUNK = 2048;   // elements that a workgroup takes at a time
