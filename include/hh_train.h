@@ -48,8 +48,10 @@ typedef struct {
 } hh_head_cfg;
 
 /* Bytes of workspace of hh_head_loss, hh_head_share_fwd and of hh_head_step, hh_head_share_bwd (either pointer may be NULL).
- * Host arithmetic only.  A step's workspace grows with tokens x vocab up to a block of 2 GiB of d beside 512 MiB of scores
- * (HH_F32: 2 GiB of both together). */
+ * Host arithmetic only.  A step's workspace grows with the tokens until a block of them has 2 GiB of d or 2 GiB of copies of its rows of
+ * x, whichever is first, beside 512 MiB of scores (HH_F32: d takes their place), 64 MiB of the products' partial sums and 17 MiB of
+ * statistics: 4.6 GiB at most (HH_F32: 4.1 GiB), where hidden is about vocab.  A loss's is 65 MiB at most (HH_F32: 2.01 GiB, with the
+ * scores of a block). */
 int hh_head_sizes(const hh_head_cfg *cfg, size_t *loss_workspace_bytes, size_t *step_workspace_bytes);
 
 /* loss[T] (fp32) of x [T, H] under the weight w [V, H] and labels[T]. */
