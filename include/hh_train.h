@@ -33,9 +33,12 @@ extern "C" {
  * holds them for a block of tokens in the workspace.
  *
  * HH_BF16: x, W, dx bfloat16; scores, statistics and losses fp32; dW fp32.  d enters the product for dx as bfloat16 (dx is rounded
- * to that at its end anyway) and the one for dW as a sum of two, 16 significant bits: dW is within 3e-6 of the exact gradient of the
- * given x and W (2-norm), where one bfloat16 number would leave 2e-3.
+ * to that at its end anyway) and the one for dW as a sum of two, which is within 2^-16 of each d: with scores of deviation 1.5 and
+ * labels some 4 above them dW was 2e-6 to 3e-6 off the exact gradient of the given x and W (2-norm), where one bfloat16 number would
+ * leave 2e-3.
  * HH_F32: everything fp32.
+ * Both: a score's own rounding, an ulp of its size in fp32, moves its p by as much of itself; the label's d = g_t (p - 1) keeps the
+ * rounding of p, up to 2^-22 g_t, also where p is nearly 1 and little else is left of d.
  *
  * Shapes: hidden a multiple of 64 (HH_BF16) or 8 (HH_F32), at most 32768; vocab 1 .. 262144, any; tokens >= 1, any; x below 2^31
  * bytes, W below 2^32 - 2^25 (HH_ERR_UNSUPPORTED_SHAPE otherwise).  The whole vocabulary is on this GPU; of a tensor-parallel share
