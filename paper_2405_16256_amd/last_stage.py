@@ -51,6 +51,7 @@ class LastStage:
         shape = (s.micro_batch, s.seq, s.hidden)
         self.acts = [torch.empty(shape, dtype=dt, device=L.DEV) for _ in self.layers]
         self.result = torch.empty(2, dtype=torch.float32, device=L.DEV)
+        self.dloss = torch.empty(s.tokens, dtype=torch.float32, device=L.DEV)   # of each token's loss: one over the tokens that count
 
     def close(self) -> None:
         torch.cuda.synchronize()
@@ -58,14 +59,16 @@ class LastStage:
 
     def gradients(self, x, labels, losses, dx) -> None:
         """Loss of each token into losses[m] and the gradients of their mean, summed over the micro-batches; dx[m] [B, S, H] is what
-        the stage before receives.  labels[m]: int64, negative where a token does not count."""
+        the stage before receives.  labels[m]: int64, negative where a token does not count; one past the vocabulary does not count either,
+        and its loss is NaN.  Tokens are counted on the device: nothing here waits for it."""
         st = L.stream_ptr()
-        scale = 1.0 / max(1, sum(int((t >= 0).sum()) for t in labels))
+        counted = sum((((t >= 0) & (t < self.head.shape[0])).sum() for t in labels), torch.zeros((), dtype=torch.int64, device=L.DEV))
+        self.dloss.copy_((1.0 / counted.clamp(min=1).double()).expand_as(self.dloss))
         for m in range(len(x)):
             ins = [x[m]] + self.acts[:-1]
             for layer, a, y, saved in zip(self.layers, ins, self.acts, self.saved):
                 hh.hh_layer_fwd(self.ctx, self.cfg, layer.wstruct, a, y, saved, self.ws, st)
-            hh.hh_head_step(self.ctx, self.head_cfg, self.acts[-1], self.head, labels[m], None, scale, losses[m], dx[m], self.dhead, m > 0,
+            hh.hh_head_step(self.ctx, self.head_cfg, self.acts[-1], self.head, labels[m], self.dloss, 1.0, losses[m], dx[m], self.dhead, m > 0,
                             self.ws, st)
             for layer, a, saved in reversed(list(zip(self.layers, ins, self.saved))):
                 hh.hh_layer_bwd(self.ctx, self.cfg, layer.wstruct, a, saved, dx[m], dx[m], layer.gstruct, m > 0, self.ws, st)
