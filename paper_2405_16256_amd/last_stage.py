@@ -30,7 +30,7 @@ class LastStage:
 
     def __init__(self, s: I.LayerShape, weights, head: np.ndarray, bf16: bool, lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, decay=0.1,
                  max_norm=1.0):
-        self.s, self.lr, self.betas, self.eps, self.max_norm, self.step_no = s, lr, (beta1, beta2), eps, max_norm, 0
+        self.s, self.lr, self.betas, self.eps, self.max_norm = s, lr, (beta1, beta2), eps, max_norm
         dt = torch.bfloat16 if bf16 else torch.float32
         self.ctx, self.cfg = hh.hh_ctx_create(0), L.cfg_of(s, bf16)
         self.layers = [L.DeviceLayer(w, s, bf16) for w in weights]
@@ -53,6 +53,18 @@ class LastStage:
         self.result = torch.empty(2, dtype=torch.float32, device=L.DEV)
         self.dloss = torch.empty(s.tokens, dtype=torch.float32, device=L.DEV)   # of each token's loss: one over the tokens that count
 
+        # updates that changed the parameters: one whose factor is not finite leaves them alone and does not count
+        self._applied, self._told, self._known = 0, torch.empty(2, dtype=torch.float32, pin_memory=True), None
+
+    @property
+    def step_no(self) -> int:
+        """Updates applied so far; waits for the norm of the last one."""
+        if self._known is not None:
+            self._known.synchronize()
+            self._applied += bool(torch.isfinite(self._told[1]))
+            self._known = None
+        return self._applied
+
     def close(self) -> None:
         torch.cuda.synchronize()
         hh.hh_ctx_destroy(self.ctx)
@@ -74,11 +86,15 @@ class LastStage:
                 hh.hh_layer_bwd(self.ctx, self.cfg, layer.wstruct, a, saved, dx[m], dx[m], layer.gstruct, m > 0, self.ws, st)
 
     def update(self) -> None:
-        """Norm and factor of all gradients into self.result, then the clipped update."""
-        self.step_no += 1
+        """Norm and factor of all gradients into self.result, then the clipped update.  The update's number in Adam's corrections depends on
+        whether the one before was applied, so this waits for that one's norm, behind which the device has this step's gradients to do."""
+        step = self.step_no + 1
         st = L.stream_ptr()
         hh.hh_grad_clip(self.ctx, self.clips, self.max_norm, self.result, self.ws, st)
-        hh.hh_adamw_step(self.ctx, hh.make_adamw_cfg(self.lr, *self.betas, self.eps, self.step_no), self.updates, self.result[1:], st)
+        self._told.copy_(self.result, non_blocking=True)
+        self._known = torch.cuda.Event()
+        self._known.record()
+        hh.hh_adamw_step(self.ctx, hh.make_adamw_cfg(self.lr, *self.betas, self.eps, step), self.updates, self.result[1:], st)
 
 
 def batch(seed: int, s: I.LayerShape, vocab: int, micro: int, bf16: bool):

@@ -46,3 +46,30 @@ def test_gradients_do_not_wait_for_the_device():
     finally:
         torch.cuda.set_sync_debug_mode(was)
     stage.close()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_step_that_is_left_out_does_not_count(bad):
+    """A gradient that is not finite: nothing changes, and the steps behind it are those of a run without it, bit for bit."""
+    stage, x, labels, losses, dx = stage_and_batch(True)
+    other = stage_and_batch(True)[0]
+    for s in (stage, other):
+        for step in range(4):
+            s.gradients(x, labels, losses, dx)
+            if step in (1, 2):
+                if s is other:
+                    continue
+                s.params[3][1].view(-1)[7] = bad
+                state = [t.clone() for t in (*s.masters, *(p for p, _, _ in s.params), *(m for pair in s.moments for m in pair))]
+                s.update()
+                assert all(torch.equal(a, b) for a, b in zip(state, (*s.masters, *(p for p, _, _ in s.params), *(m for pair in s.moments for m in pair))))
+                continue
+            s.update()
+        assert s.step_no == 2
+    for a, b in zip(stage.masters, other.masters):
+        assert torch.equal(a, b)
+    for a, b in zip(stage.moments, other.moments):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert all(torch.equal(a[0], b[0]) for a, b in zip(stage.params, other.params))
+    stage.close()
+    other.close()
