@@ -215,9 +215,10 @@ hipError_t head_rows(const HeadTokens& t, const float2* stats, int slots, float*
 }
 
 // ------------------------------------------------------------------ gradient of the scores
-// Of longer rows.  Bound by HBM: 2048 rows of 32000 91 us, 5.9 TB/s of scores in and d out.  A workgroup turns 1024 scores of a
+// Of longer rows.  Bound by HBM: 2048 rows of 32000 86 us, 6.1 TB/s of scores in and d out.  A workgroup turns 1024 scores of a
 // row into d; columns N .. ldz-1 become zeros, and so do rows that do not count, whatever their scores are.  The workgroups past
-// those of the scores copy the row's x.  p = exp(z - m) / S from norm, exp(z - lse) where that is null.
+// those of the scores copy the row's x.  p = exp(z - m) / S from norm, exp(z - lse) where that is null.  The scores are asked for, 16
+// bytes a lane, in front of what the row has in common: left to the compiler they wait for it, in three pieces (101 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_head_grad(HeadTokens t, const float* z, int ldz, const float2* __restrict__ norm, const float* __restrict__ lse,
                                                    T* d, int lo_rows, const T* __restrict__ x, T* __restrict__ xs, int H, int z_wgs) {
@@ -235,10 +236,11 @@ __global__ __launch_bounds__(256) void k_head_grad(HeadTokens t, const float* z,
     if (col >= ldz) return;
     float f[4] = {0.f, 0.f, 0.f, 0.f};
     if (counts && col < t.N) {
+        Vec<float>::load(z + (size_t)row * ldz + col, f);
+        __builtin_amdgcn_sched_barrier(0);
         const float2 of = norm ? norm[row] : make_float2(lse[row], 1.f);
         const float g = t.dloss ? t.scale * t.dloss[row] : t.scale;
         const int64_t column = label - t.first;
-        Vec<float>::load(z + (size_t)row * ldz + col, f);
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const float p = __builtin_amdgcn_exp2f((f[e] - of.x) * LOG2_E) * of.y;
