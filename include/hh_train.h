@@ -34,8 +34,8 @@ extern "C" {
  *
  * HH_BF16: x, W, dx bfloat16; scores, statistics and losses fp32; dW fp32.  d enters the product for dx as bfloat16 (dx is rounded
  * to that at its end anyway) and the one for dW as a sum of two, which is within 2^-16 of each d: with scores of deviation 1.5 and
- * labels some 4 above them dW was 2e-6 to 3e-6 off the exact gradient of the given x and W (2-norm), where one bfloat16 number would
- * leave 2e-3.
+ * labels some 4 above them dW was 1.4e-6 to 2.2e-6 off the exact gradient of the given x and W (2-norm), where products in fp32 leave
+ * 4e-7 to 8e-7 and one bfloat16 number would leave 2e-3.
  * HH_F32: everything fp32.
  * Both: a score's own rounding, an ulp of its size in fp32, moves its p by as much of itself; the label's d = g_t (p - 1) keeps the
  * rounding of p, up to 2^-22 g_t, also where p is nearly 1 and little else is left of d.

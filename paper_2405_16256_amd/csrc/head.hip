@@ -40,9 +40,10 @@ __device__ __forceinline__ void put_x(const T* __restrict__ x, T* __restrict__ x
 // ------------------------------------------------------------------ whole rows
 // All scores of a row in the registers of one workgroup: read once for the largest, the sum, the loss and d.  Bound by HBM
 // (8 bytes a score in a step), by launches on small problems, of which it is one where the statistics and d apart are two, in fp32
-// three (head steps of bf16 200 tokens, hidden 512, vocabulary 2000: 26.5 -> 23.8 us; fp32 128, 256, 1000: 23.2 -> 18.6; 700,
-// 1024, 8001: 320 -> 311).  In bf16, whose statistics come with the product, it loses past 16384 columns: a workgroup of 1024 threads
-// with 32 scores each has a CU to itself, and nothing is stored while it loads (2048 rows of 32000: 104 -> 114 us).
+// three (head steps of fp32 128 tokens, hidden 256, vocabulary 1000: 25.7 -> 18.1 us; 700, 1024, 8001: 317 -> 308; 700, 512, 30000: 598 -> 584;
+// bf16 200, 512, 2000: 24.6 -> 22.0; 700, 512, 8191: 56.9 -> 53.7).  In bf16, whose statistics come with the product, it gains nothing
+// between 8192 and 16384 columns (700 tokens, 512, 16384: 99.3 -> 99.0; 8192 tokens: 837 -> 864) and loses past that: a workgroup of 1024
+// threads with 32 scores each has a CU to itself, and nothing is stored while it loads (2048 rows of 32000: 95 us apart, 114 whole).
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void k_head_row(HeadTokens t, const float* z, int ldz, float* __restrict__ loss, T* d, int lo_rows,
                                                       const T* __restrict__ x, T* __restrict__ xs, int H) {
