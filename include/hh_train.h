@@ -103,8 +103,9 @@ int hh_grad_clip(hh_ctx *ctx, int n, const hh_clip_tensor *tensors, float max_no
  *     g' = factor * g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
  *     p = p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + decay p)
  * in fp32, with constants formed in fp64.  factor: device, fp32, one value (result + 1 of hh_grad_clip: clipped gradients need
- * not be written and read again), or NULL for 1; a factor that is not finite leaves every tensor as it is.  A bfloat16 parameter has an fp32 master
- * copy, which is p above, and receives p rounded; an fp32 parameter is its own master copy (master NULL).  step counts from 1.
+ * not be written and read again), or NULL for 1; a factor that is not finite leaves every tensor as it is, and that call
+ * was no step: the next one has the same number.  A bfloat16 parameter has an fp32 master copy, which is p above, and receives p
+ * rounded; an fp32 parameter is its own master copy (master NULL).  step counts from 1.
  * Pointers, tensors, n and counts as in hh_grad_clip. */
 typedef struct {
     void *param;
