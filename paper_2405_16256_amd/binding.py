@@ -27,12 +27,16 @@ HH_F32 = 0
 HH_BF16 = 1
 HH_STATIC_SCRATCH_BYTES = 128 << 20
 HH_CLIP_WORKSPACE_BYTES = 8192
+HH_MX_NONE, HH_MX_E4M3, HH_MX_E2M1 = 0, 1, 2
+HH_MX_PAD = 256
 
 WEIGHT_FIELDS = ("g_attn", "wq", "wk", "wv", "wo", "g_mlp", "w_gate", "w_up", "w_down")
 EXPORTS = ("hh_last_error", "hh_ctx_create", "hh_ctx_destroy", "hh_ctx_reserve", "hh_layer_flops", "hh_layer_sizes",
            "hh_saved_layout_of", "hh_layer_fwd", "hh_layer_fwd_noalloc", "hh_layer_bwd", "hh_stage_sizes", "hh_stage_step", "hh_stage_step_1f1b", "hh_layer_profile", "hh_trace_begin",
            "hh_trace_end", "hh_sim_pipeline", "hh_sim_weighted_mean", "hh_plan_layers", "hh_plan_order", "hh_plan_cluster",
-           "hh_head_sizes", "hh_head_loss", "hh_head_step", "hh_head_share_fwd", "hh_head_share_bwd", "hh_grad_clip", "hh_adamw_step")
+           "hh_head_sizes", "hh_head_loss", "hh_head_step", "hh_head_share_fwd", "hh_head_share_bwd", "hh_grad_clip", "hh_adamw_step",
+           "hh_dropout", "hh_mx_sizes", "hh_mx_quantise", "hh_mx_values", "hh_add_norm_fwd", "hh_add_norm_sizes", "hh_add_norm_bwd",
+           "hh_mx_product_sizes", "hh_mx_product")
 TRACE_KINDS = ("gemm_nt", "gemm_nn", "gemm_tn", "attn_fwd", "attn_bwd", "elementwise")
 
 
@@ -109,6 +113,23 @@ class hh_adamw_cfg(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64)]
 
 
+class hh_dropout_cfg(C.Structure):
+    _fields_ = [("seed", C.c_uint64), ("offset", C.c_uint64), ("step", C.c_void_p), ("p", C.c_double)]
+
+
+class hh_mx_tensor(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class hh_add_norm_cfg(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("hidden", C.c_int32), ("eps", C.c_float), ("dtype", C.c_int32), ("format", C.c_int32)]
+
+
+class hh_mx_product_cfg(C.Structure):
+    _fields_ = [("m", C.c_int32), ("n", C.c_int32), ("k", C.c_int32), ("a_format", C.c_int32), ("b_format", C.c_int32), ("dtype", C.c_int32),
+                ("ldc", C.c_int64)]
+
+
 class HHError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__("hh error %d: %s" % (code, msg))
@@ -121,6 +142,7 @@ def _load() -> C.CDLL:
                           "(there is no fallback path)" % _LIB_PATH)
     lib = C.CDLL(_LIB_PATH)
     vp, i, sz = C.c_void_p, C.c_int, C.POINTER(C.c_size_t)
+    i32, i64, mxp, anp = C.c_int32, C.c_int64, C.POINTER(hh_mx_tensor), C.POINTER(hh_add_norm_cfg)
     cfgp, wp, gp = C.POINTER(hh_layer_cfg), C.POINTER(hh_layer_weights), C.POINTER(hh_layer_grads)
     lib.hh_last_error.restype = C.c_char_p
     lib.hh_last_error.argtypes = []
@@ -157,6 +179,15 @@ def _load() -> C.CDLL:
         "hh_head_share_bwd": [vp, C.POINTER(hh_head_cfg), vp, vp, vp, C.c_int32, vp, vp, C.c_float, vp, vp, i, vp, vp],
         "hh_grad_clip": [vp, i, C.POINTER(hh_clip_tensor), C.c_float, vp, vp, vp],
         "hh_adamw_step": [vp, C.POINTER(hh_adamw_cfg), i, C.POINTER(hh_adamw_tensor), vp, vp],
+        "hh_dropout": [vp, C.POINTER(hh_dropout_cfg), i64, i64, i32, vp, i64, vp, i64, vp],
+        "hh_mx_sizes": [i32, i64, i64, sz, sz],
+        "hh_mx_quantise": [vp, i64, i64, i32, vp, i64, i32, mxp, mxp, vp],
+        "hh_mx_values": [vp, i64, i64, i32, mxp, i32, vp, i64, vp],
+        "hh_add_norm_fwd": [vp, anp, C.POINTER(hh_dropout_cfg), vp, vp, vp, vp, vp, mxp, vp],
+        "hh_add_norm_sizes": [anp, sz],
+        "hh_add_norm_bwd": [vp, anp, C.POINTER(hh_dropout_cfg), vp, vp, vp, vp, vp, vp, vp, i, vp, vp],
+        "hh_mx_product_sizes": [C.POINTER(hh_mx_product_cfg), sz],
+        "hh_mx_product": [vp, C.POINTER(hh_mx_product_cfg), mxp, mxp, vp, i, vp, vp],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -449,3 +480,72 @@ def make_adamw_cfg(lr, beta1=0.9, beta2=0.95, eps=1e-8, step=1) -> hh_adamw_cfg:
 def hh_adamw_step(ctx, cfg: hh_adamw_cfg, tensors, factor=None, stream=0) -> None:
     """tensors: of make_adamw_tensors; factor: one fp32 value on the device (result[1:] of hh_grad_clip) or None."""
     _check(lib.hh_adamw_step(ctx, C.byref(cfg), len(tensors), tensors, _ptr(factor), stream))
+
+
+# ---------------------------------------------------------------- residual path and microscaled products
+def _ref(struct):
+    return None if struct is None else C.byref(struct)
+
+
+def make_dropout(p, seed, offset=0, step=None) -> hh_dropout_cfg:
+    """step: a tensor of one int64 on the device that is added to offset when the kernel runs, or None.  It has to stay alive."""
+    return hh_dropout_cfg(seed, offset, _ptr(step), p)
+
+
+def hh_dropout(ctx, drop: hh_dropout_cfg, rows, cols, dtype, x, ldx, y, ldy, stream=0) -> None:
+    _check(lib.hh_dropout(ctx, _ref(drop), rows, cols, dtype, _ptr(x), ldx, _ptr(y), ldy, stream))
+
+
+def make_mx(codes, scales) -> hh_mx_tensor:
+    """A packed tensor in the caller's buffers (of hh_mx_sizes bytes).  It holds addresses: the buffers have to stay alive."""
+    return hh_mx_tensor(_ptr(codes), _ptr(scales))
+
+
+def hh_mx_sizes(format, rows, k) -> tuple[int, int]:
+    """-> bytes of (codes, scales)"""
+    a, b = C.c_size_t(), C.c_size_t()
+    _check(lib.hh_mx_sizes(format, rows, k, C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def hh_mx_quantise(ctx, rows, cols, dtype, x, ldx, format, by_row: hh_mx_tensor | None, by_column: hh_mx_tensor | None, stream=0) -> None:
+    _check(lib.hh_mx_quantise(ctx, rows, cols, dtype, _ptr(x), ldx, format, _ref(by_row), _ref(by_column), stream))
+
+
+def hh_mx_values(ctx, rows, k, format, q: hh_mx_tensor, dtype, y, ldy, stream=0) -> None:
+    _check(lib.hh_mx_values(ctx, rows, k, format, _ref(q), dtype, _ptr(y), ldy, stream))
+
+
+def make_add_norm_cfg(rows, hidden, eps=1e-5, dtype=HH_BF16, format=HH_MX_NONE) -> hh_add_norm_cfg:
+    return hh_add_norm_cfg(rows, hidden, eps, dtype, format)
+
+
+def hh_add_norm_fwd(ctx, cfg: hh_add_norm_cfg, drop: hh_dropout_cfg | None, x, b, g, h, xn, q: hh_mx_tensor | None, stream=0) -> None:
+    _check(lib.hh_add_norm_fwd(ctx, C.byref(cfg), _ref(drop), _ptr(x), _ptr(b), _ptr(g), _ptr(h), _ptr(xn), _ref(q), stream))
+
+
+def hh_add_norm_sizes(cfg: hh_add_norm_cfg) -> int:
+    """-> workspace bytes of hh_add_norm_bwd"""
+    a = C.c_size_t()
+    _check(lib.hh_add_norm_sizes(C.byref(cfg), C.byref(a)))
+    return a.value
+
+
+def hh_add_norm_bwd(ctx, cfg: hh_add_norm_cfg, drop: hh_dropout_cfg | None, h, g, dxn, dh, dx, db, dg, accumulate, workspace, stream=0) -> None:
+    _check(lib.hh_add_norm_bwd(ctx, C.byref(cfg), _ref(drop), _ptr(h), _ptr(g), _ptr(dxn), _ptr(dh), _ptr(dx), _ptr(db), _ptr(dg),
+                               int(accumulate), _ptr(workspace), stream))
+
+
+def make_mx_product_cfg(m, n, k, a_format, b_format, dtype=HH_BF16, ldc=None) -> hh_mx_product_cfg:
+    return hh_mx_product_cfg(m, n, k, a_format, b_format, dtype, n if ldc is None else ldc)
+
+
+def hh_mx_product_sizes(cfg: hh_mx_product_cfg) -> int:
+    """-> workspace bytes"""
+    a = C.c_size_t()
+    _check(lib.hh_mx_product_sizes(C.byref(cfg), C.byref(a)))
+    return a.value
+
+
+def hh_mx_product(ctx, cfg: hh_mx_product_cfg, a: hh_mx_tensor, b: hh_mx_tensor, c, accumulate, workspace, stream=0) -> None:
+    _check(lib.hh_mx_product(ctx, C.byref(cfg), _ref(a), _ref(b), _ptr(c), int(accumulate), _ptr(workspace), stream))

@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhh.so")
 SOURCES = ["hh_api.cpp", "predictor.cpp", "elementwise.hip", "gemm_f32.hip", "gemm_f32_long_k.hip", "gemm_bf16.hip", "attn_f32.hip", "attn_bf16.hip", "scratch.hip",
-           "hh_train.cpp", "head.hip", "tensors.hip"]
+           "hh_train.cpp", "head.hip", "tensors.hip", "hh_mx.cpp", "residual.hip", "mx_pack.hip", "mx_product.hip"]
 # Packed fp32 instructions are kept out of the generated code on purpose.  Up to 14 words of a kernel's arguments, as far as the first
 # struct among them, arrive in registers instead of being loaded by every workgroup: the attention kernels' pointers, 3 or 4 words
 # of the GEMMs on rings, none of the 256x256 ones.  Steps of hidden 256, 128 tokens: fp32 78.9 -> 77.3 us, 4 bf16 layers of 8

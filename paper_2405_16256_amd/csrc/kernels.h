@@ -192,4 +192,26 @@ hipError_t clip_scale(const ClipList& l, const double* slots, int n_slots, float
 // stream: the tensors of all launches together are past LIST_CACHE
 hipError_t adamw(const AdamwList& l, const AdamwHyper& h, const float* factor, bool stream, hipStream_t st);
 
+// ---- residual path and microscaled formats (residual.hip, mx_pack.hip, mx_product.hip)
+enum { MX_NONE = 0, MX_E4M3 = 1, MX_E2M1 = 2 };
+constexpr int MX_PAD = 256;
+inline long mx_width(long k) { return (k + MX_PAD - 1) / MX_PAD * MX_PAD; }
+// dropped: of 65536 values, scale: of the others (nothing is dropped at 0)
+struct Drop { uint64_t seed, offset; const uint64_t* step; uint32_t dropped; float scale; };
+// A packed tensor of rows of `width` codes, a multiple of MX_PAD
+struct MxRows { uint8_t* codes; uint8_t* scales; };
+hipError_t dropout(int dtype, const Drop& d, long rows, long cols, const void* x, long ldx, void* y, long ldy, hipStream_t st);
+hipError_t add_norm_fwd(int dtype, const Drop& d, int rows, int hidden, float eps, const void* x, const void* b, const void* g, void* h, void* xn,
+                        int format, const MxRows& q, hipStream_t st);
+// partial: add_norm_partial_rows() rows of `hidden` sums for dg, which is not written where it is null
+int add_norm_partial_rows(int rows, int hidden);
+hipError_t add_norm_bwd(int dtype, const Drop& d, int rows, int hidden, float eps, const void* h, const void* g, const void* dxn, const void* dh,
+                        void* dx, void* db, float* dg, int accumulate, float* partial, hipStream_t st);
+hipError_t mx_quantise(int dtype, long rows, long cols, const void* x, long ldx, int format, const MxRows& by_row, const MxRows& by_column,
+                       hipStream_t st);
+hipError_t mx_values(int dtype, long rows, long k, int format, const MxRows& q, void* y, long ldy, hipStream_t st);
+struct MxProduct { int M, N, K; int fa, fb; MxRows a, b; void* C; long ldc; int f32, accumulate; };
+size_t mx_product_workspace(const MxProduct& p);
+hipError_t mx_product(const MxProduct& p, void* ws, hipStream_t st);
+
 }  // namespace hh

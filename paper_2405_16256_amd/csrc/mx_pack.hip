@@ -1,0 +1,165 @@
+// Packing to microscaled formats and back.
+#include "mx.h"
+
+namespace hh {
+
+// ------------------------------------------------------------------ by row
+// Eight values a lane, four lanes a block.
+template <typename T, int F>
+__global__ __launch_bounds__(256) void k_pack_rows(int chunks, Divisor per_row, int cols, const T* __restrict__ x, long ldx, uint8_t* __restrict__ codes,
+                                                    uint8_t* __restrict__ scales) {
+    const int i = (int)(blockIdx.x * 256u + threadIdx.x);
+    if (i >= chunks) return;   // whole rows of a multiple of 32 chunks
+    int row = i;
+    const int group = split_off(row, per_row), n = cols - 8 * group;
+    Eight<T> e{};
+    if (n > 0) e.load(x + row * ldx + 8L * group, n);
+    float v[8];
+    e.widen(v);
+    const uint32_t byte = scale_byte<F>(quad_max(magnitude8(v)));
+    Codes8<F> q;
+    q.set(v, byte);
+    q.store(codes, (size_t)i);
+    if ((group & 3) == 0) scales[(size_t)i >> 2] = (uint8_t)byte;
+}
+
+// ------------------------------------------------------------------ by column, and both
+// A lane takes 8 columns (fp32: 4) of a block of 32 rows in registers, 8 lanes the columns beside them and 8 the row blocks below: a load covers 128
+// bytes of 8 rows, and the blocks along columns need no exchange at all; stores of a column's codes cover 8 blocks.
+template <typename T> constexpr int columns_each() { return sizeof(T) == 2 ? 8 : 4; }
+
+template <typename T, int F, bool ROWS>
+__global__ __launch_bounds__(256) void k_pack_columns(long rows, int cols, const T* __restrict__ x, long ldx, int width, uint8_t* __restrict__ codes,
+                                                       uint8_t* __restrict__ scales, long column_width, uint8_t* __restrict__ column_codes,
+                                                       uint8_t* __restrict__ column_scales, Divisor tiles_across) {
+    constexpr int N = columns_each<T>(), BITS = F == MX_E4M3 ? 8 : 4;
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    int down = (int)blockIdx.x;
+    const int across = split_off(down, tiles_across);
+    const int col0 = across * (4 * 8 * N) + wave * (8 * N) + (lane & 7) * N;
+    const long block = (long)down * 8 + (lane >> 3), row0 = block * 32;
+    const int n = cols - col0;
+    Few<T, N> raw[32];
+#pragma unroll
+    for (int r = 0; r < 32; r++) {
+        raw[r] = Few<T, N>{};
+        if (n > 0 && row0 + r < rows) raw[r].load(x + (row0 + r) * ldx + col0, n);
+    }
+    if (ROWS && col0 < width) {
+#pragma unroll
+        for (int r = 0; r < 32; r++) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = i < N ? raw[r].at(i % N) : 0.f;
+            uint32_t m = quad_max(magnitude8(v));
+            if (N == 4) m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xF, 0xF, true));   // the other four of eight lanes
+            const uint32_t byte = scale_byte<F>(m);
+            Codes8<F> q;
+            q.set(v, byte);
+            if (row0 + r < rows) {
+                uint8_t* const to = codes + ((size_t)(row0 + r) * width + col0) * BITS / 8;
+                if constexpr (N == 8) q.store(to, 0);
+                else if constexpr (F == MX_E4M3) *reinterpret_cast<uint32_t*>(to) = q.w.x;
+                else *reinterpret_cast<uint16_t*>(to) = (uint16_t)q.w;
+                if ((col0 & 31) == 0) scales[(size_t)(row0 + r) * (width / MX_BLOCK) + (col0 >> 5)] = (uint8_t)byte;
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+        if (j >= n) continue;
+        uint32_t m = 0;
+#pragma unroll
+        for (int r = 0; r < 32; r++) m = max(m, __float_as_uint(raw[r].at(j)) & 0x7FFFFFFFu);
+        const uint32_t byte = scale_byte<F>(m);
+        uint32_t w[BITS];   // 32 codes
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = raw[8 * k + i].at(j);
+            Codes8<F> q;
+            q.set(v, byte);
+            if constexpr (F == MX_E4M3) { w[2 * k] = q.w.x; w[2 * k + 1] = q.w.y; }
+            else w[k] = q.w;
+        }
+        uint4* const to = reinterpret_cast<uint4*>(column_codes + ((size_t)(col0 + j) * column_width + row0) * BITS / 8);
+        to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        if constexpr (BITS == 8) to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        column_scales[(size_t)(col0 + j) * (column_width / MX_BLOCK) + block] = (uint8_t)byte;
+    }
+}
+
+template <typename T, int F>
+static hipError_t quantise(long rows, long cols, const void* x, long ldx, const MxRows& by_row, const MxRows& by_column, hipStream_t st) {
+    const int width = (int)mx_width(cols);
+    if (!by_column.codes) {
+        const int chunks = (int)(rows * (width / 8));
+        k_pack_rows<T, F><<<((unsigned)chunks + 255u) / 256u, 256, 0, st>>>(chunks, divisor(width / 8), (int)cols, (const T*)x, ldx, by_row.codes,
+                                                                           by_row.scales);
+        return hipGetLastError();
+    }
+    const long column_width = mx_width(rows);
+    const int across = by_row.codes ? width / (32 * columns_each<T>()) : (int)((cols + 32 * columns_each<T>() - 1) / (32 * columns_each<T>()));
+    const unsigned grid = (unsigned)(across * (column_width / 256));
+    if (by_row.codes)
+        k_pack_columns<T, F, true><<<grid, 256, 0, st>>>(rows, (int)cols, (const T*)x, ldx, width, by_row.codes, by_row.scales, column_width,
+                                                         by_column.codes, by_column.scales, divisor(across));
+    else
+        k_pack_columns<T, F, false><<<grid, 256, 0, st>>>(rows, (int)cols, (const T*)x, ldx, width, nullptr, nullptr, column_width, by_column.codes,
+                                                          by_column.scales, divisor(across));
+    return hipGetLastError();
+}
+hipError_t mx_quantise(int dtype, long rows, long cols, const void* x, long ldx, int format, const MxRows& by_row, const MxRows& by_column,
+                       hipStream_t st) {
+    if (dtype == DT_BF16)
+        return format == MX_E4M3 ? quantise<bf16_t, MX_E4M3>(rows, cols, x, ldx, by_row, by_column, st)
+                                 : quantise<bf16_t, MX_E2M1>(rows, cols, x, ldx, by_row, by_column, st);
+    return format == MX_E4M3 ? quantise<float, MX_E4M3>(rows, cols, x, ldx, by_row, by_column, st)
+                             : quantise<float, MX_E2M1>(rows, cols, x, ldx, by_row, by_column, st);
+}
+
+// ------------------------------------------------------------------ values
+template <typename T, int F>
+__global__ __launch_bounds__(256) void k_values(int chunks, Divisor per_row, int k, int width, const uint8_t* __restrict__ codes,
+                                                 const uint8_t* __restrict__ scales, T* __restrict__ y, long ldy) {
+    const int i = (int)(blockIdx.x * 256u + threadIdx.x);
+    if (i >= chunks) return;
+    int row = i;
+    const int group = split_off(row, per_row);
+    const size_t at = (size_t)row * (width / 8) + group;
+    const float s = scale_value(scales[at >> 2]);
+    typedef float f32x2v __attribute__((ext_vector_type(2)));
+    float v[8];
+    if constexpr (F == MX_E4M3) {
+        const uint2 w = reinterpret_cast<const uint2*>(codes)[at];
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            const f32x2v a = __builtin_amdgcn_cvt_pk_f32_fp8((int)(q ? w.y : w.x), false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)(q ? w.y : w.x), true);
+            v[4 * q] = a[0]; v[4 * q + 1] = a[1]; v[4 * q + 2] = b[0]; v[4 * q + 3] = b[1];
+        }
+    } else {
+        const uint32_t w = reinterpret_cast<const uint32_t*>(codes)[at];
+        const f32x2v a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
+        const f32x2v c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
+        v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1]; v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] *= s;
+    Eight<T> e;
+    e.round(v);
+    e.store(y + row * ldy + 8L * group, k - 8 * group);
+}
+
+hipError_t mx_values(int dtype, long rows, long k, int format, const MxRows& q, void* y, long ldy, hipStream_t st) {
+    const int per_row = (int)((k + 7) / 8), chunks = (int)(rows * per_row), width = (int)mx_width(k);
+    const unsigned grid = ((unsigned)chunks + 255u) / 256u;
+    auto run = [&](auto kern, auto* to) {
+        kern<<<grid, 256, 0, st>>>(chunks, divisor(per_row), (int)k, width, q.codes, q.scales, to, ldy);
+        return hipGetLastError();
+    };
+    if (dtype == DT_BF16) return format == MX_E4M3 ? run(k_values<bf16_t, MX_E4M3>, (bf16_t*)y) : run(k_values<bf16_t, MX_E2M1>, (bf16_t*)y);
+    return format == MX_E4M3 ? run(k_values<float, MX_E4M3>, (float*)y) : run(k_values<float, MX_E2M1>, (float*)y);
+}
+
+}  // namespace hh

@@ -1,0 +1,347 @@
+// Dropout, and the residual's addition with its norm: forward and backward.  All of them stream their tensors once.
+#include "mx.h"
+
+namespace hh {
+
+// ------------------------------------------------------------------ dropout
+template <typename T>
+__global__ __launch_bounds__(256) void k_dropout(Drop d, int chunks, Divisor per_row, int cols, const T* x, long ldx, T* y, long ldy) {
+    const int i = (int)(blockIdx.x * 256u + threadIdx.x);
+    if (i >= chunks) return;
+    int row = i;
+    const int group = split_off(row, per_row), n = cols - 8 * group;
+    const long at = 8L * group;
+    Eight<T> e;
+    e.load(x + row * ldx + at, n);
+    float v[8];
+    e.widen(v);
+    drop8(d, drop_offset(d), (uint32_t)group, (uint32_t)row, v);
+    e.round(v);
+    e.store(y + row * ldy + at, n);
+}
+
+hipError_t dropout(int dtype, const Drop& d, long rows, long cols, const void* x, long ldx, void* y, long ldy, hipStream_t st) {
+    const int per_row = (int)((cols + 7) / 8), chunks = (int)(rows * per_row);
+    const unsigned grid = ((unsigned)chunks + 255u) / 256u;
+    if (dtype == DT_BF16)
+        k_dropout<bf16_t><<<grid, 256, 0, st>>>(d, chunks, divisor(per_row), (int)cols, (const bf16_t*)x, ldx, (bf16_t*)y, ldy);
+    else
+        k_dropout<float><<<grid, 256, 0, st>>>(d, chunks, divisor(per_row), (int)cols, (const float*)x, ldx, (float*)y, ldy);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ residual and norm
+// W waves a row, CH chunks of eight values a lane: chunk t + 64 W c.  Four rows to a workgroup where a wave takes one.
+template <int W> constexpr int row_threads() { return W == 1 ? 256 : 64 * W; }
+template <int W> constexpr int rows_each() { return W == 1 ? 4 : 1; }
+
+template <typename T, int W, int CH>
+__global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int rows, int hidden, int width, float eps, const T* x, const T* b,
+                                                                     const T* __restrict__ g, T* h, T* xn, int format, uint8_t* codes, uint8_t* scales) {
+    __shared__ float red[W];
+    const int t = (int)threadIdx.x & (64 * W - 1);
+    const int row = (int)blockIdx.x * rows_each<W>() + (W == 1 ? (int)threadIdx.x >> 6 : 0);
+    if (row >= rows) return;   // one wave a row: no barrier follows
+    const long base = (long)row * hidden;
+    Eight<T> rx[CH], rb[CH], rg[CH];
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+        const int at = 8 * (t + 64 * W * c), n = hidden - at;
+        rx[c] = Eight<T>{};
+        rb[c] = Eight<T>{};
+        rg[c] = Eight<T>{};
+        if (n > 0) {
+            rx[c].load(x + base + at, n);
+            if (b) rb[c].load(b + base + at, n);
+            rg[c].load(g + at, n);
+        }
+    }
+    const uint64_t offset = b && d.dropped ? drop_offset(d) : 0;
+    float v[CH][8], ss = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+        const int group = t + 64 * W * c, n = hidden - 8 * group;
+        rx[c].widen(v[c]);
+        if (b && n > 0) {
+            float u[8];
+            rb[c].widen(u);
+            if (d.dropped) drop8(d, offset, (uint32_t)group, (uint32_t)row, u);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[c][i] += u[i];
+            rx[c].round(v[c]);
+            rx[c].store(h + base + 8 * group, n);
+            rx[c].widen(v[c]);   // the norm is of the sum as it is kept
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) ss = fmaf(v[c][i], v[c][i], ss);
+    }
+    ss = W == 1 ? wave_sum(ss) : block_sum<W>(ss, red);
+    const float r = 1.0f / sqrtf(ss / (float)hidden + eps);
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+        const int group = t + 64 * W * c, n = hidden - 8 * group;
+        float u[8];
+        rg[c].widen(u);
+#pragma unroll
+        for (int i = 0; i < 8; i++) u[i] = i < n ? v[c][i] * r * u[i] : 0.f;
+        if (xn && n > 0) {
+            Eight<T> e;
+            e.round(u);
+            e.store(xn + base + 8 * group, n);
+        }
+        if (format != MX_NONE && 8 * group < width) {   // whole blocks of 32: the four lanes of one are here together
+            const uint32_t m = quad_max(magnitude8(u));
+            uint32_t byte;
+            if (format == MX_E4M3) {
+                Codes8<MX_E4M3> q;
+                q.set(u, byte = scale_byte<MX_E4M3>(m));
+                q.store(codes + (size_t)row * width, group);
+            } else {
+                Codes8<MX_E2M1> q;
+                q.set(u, byte = scale_byte<MX_E2M1>(m));
+                q.store(codes + (size_t)row * (width / 2), group);
+            }
+            if ((group & 3) == 0) scales[(size_t)row * (width / MX_BLOCK) + (group >> 2)] = (uint8_t)byte;
+        }
+    }
+}
+
+template <typename T>
+static hipError_t fwd(const Drop& d, int rows, int hidden, float eps, const void* x, const void* b, const void* g, void* h, void* xn, int format,
+                      const MxRows& q, hipStream_t st) {
+    const int width = format == MX_NONE ? 0 : (int)mx_width(hidden), chunks = format == MX_NONE ? (hidden + 7) / 8 : width / 8;
+    auto run = [&](auto kern, int each, int threads) {
+        kern<<<(rows + each - 1) / each, threads, 0, st>>>(d, rows, hidden, width, eps, (const T*)x, (const T*)b, (const T*)g, (T*)h, (T*)xn, format,
+                                                           q.codes, q.scales);
+        return hipGetLastError();
+    };
+#define HH_SHAPE(W, CH) if (chunks <= 64 * W * CH) return run(k_add_norm_fwd<T, W, CH>, rows_each<W>(), row_threads<W>())
+    HH_SHAPE(1, 1); HH_SHAPE(1, 2); HH_SHAPE(1, 4);
+    HH_SHAPE(4, 2); HH_SHAPE(4, 3); HH_SHAPE(4, 4); HH_SHAPE(4, 6);
+    HH_SHAPE(16, 2); HH_SHAPE(16, 4);
+#undef HH_SHAPE
+    return hipErrorInvalidValue;
+}
+hipError_t add_norm_fwd(int dtype, const Drop& d, int rows, int hidden, float eps, const void* x, const void* b, const void* g, void* h, void* xn,
+                        int format, const MxRows& q, hipStream_t st) {
+    return dtype == DT_BF16 ? fwd<bf16_t>(d, rows, hidden, eps, x, b, g, h, xn, format, q, st)
+                            : fwd<float>(d, rows, hidden, eps, x, b, g, h, xn, format, q, st);
+}
+
+// ------------------------------------------------------------------ gradients
+// One row's share of dx, db and dg: eight values of h (a), dxn (u), g (w) and dh (o, which becomes dx).
+__device__ __forceinline__ void norm_grad8(const float* a, const float* u, const float* w, float* o, float* sum, float r, float k) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        sum[i] = fmaf(u[i], a[i] * r, sum[i]);
+        o[i] = fmaf(r, fmaf(-a[i], k, u[i] * w[i]), o[i]);
+    }
+}
+// The two sums of a row over the waves of a workgroup; `red` is taken in turn, so that a row needs one barrier.
+template <int W>
+__device__ __forceinline__ void row_sums(float& ss, float& dot, float (&red)[2][W]) {
+    ss = wave_sum(ss);
+    dot = wave_sum(dot);
+    if (W > 1) {
+        if ((threadIdx.x & 63) == 0) { red[0][threadIdx.x >> 6] = ss; red[1][threadIdx.x >> 6] = dot; }
+        __syncthreads();
+        ss = dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; i++) { ss += red[0][i]; dot += red[1][i]; }
+    }
+}
+
+// Workgroups (waves, where a wave takes a row) walk rows p, p + P, ... and keep their sums for dg in registers; partial[p] of P.
+template <typename T, int W, int CH>
+__global__ __launch_bounds__(row_threads<W>()) void k_add_norm_bwd(Drop d, int rows, int hidden, int parts, float eps, const T* h, const T* __restrict__ g,
+                                                                     const T* dxn, const T* dh, T* dx, T* db, float* __restrict__ partial) {
+    __shared__ float red[2][2][W];
+    const int t = (int)threadIdx.x & (64 * W - 1);
+    const int p = (int)blockIdx.x * rows_each<W>() + (W == 1 ? (int)threadIdx.x >> 6 : 0);
+    if (p >= parts) return;
+    const uint64_t offset = db && d.dropped ? drop_offset(d) : 0;
+    Eight<T> rg[CH];
+    float sum[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+        const int at = 8 * (t + 64 * W * c), n = hidden - at;
+        rg[c] = Eight<T>{};
+        if (n > 0) rg[c].load(g + at, n);
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum[c][i] = 0.f;
+    }
+    int turn = 0;
+    for (int row = p; row < rows; row += parts, turn ^= 1) {
+        const long base = (long)row * hidden;
+        Eight<T> rh[CH], ru[CH], rd[CH];
+#pragma unroll
+        for (int c = 0; c < CH; c++) {
+            const int at = 8 * (t + 64 * W * c), n = hidden - at;
+            rh[c] = Eight<T>{};
+            ru[c] = Eight<T>{};
+            rd[c] = Eight<T>{};
+            if (n > 0) {
+                rh[c].load(h + base + at, n);
+                ru[c].load(dxn + base + at, n);
+                if (dh) rd[c].load(dh + base + at, n);
+            }
+        }
+        float ss = 0.f, dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; c++) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float a = rh[c].at(i);
+                ss = fmaf(a, a, ss);
+                dot = fmaf(ru[c].at(i) * rg[c].at(i), a, dot);
+            }
+        }
+        row_sums<W>(ss, dot, red[turn]);
+        const float r = 1.0f / sqrtf(ss / (float)hidden + eps), k = r * r * (dot / (float)hidden);
+#pragma unroll
+        for (int c = 0; c < CH; c++) {
+            const int group = t + 64 * W * c, n = hidden - 8 * group;
+            if (n <= 0) continue;
+            float a[8], u[8], w[8], o[8];
+            rh[c].widen(a);
+            ru[c].widen(u);
+            rg[c].widen(w);
+            rd[c].widen(o);
+            norm_grad8(a, u, w, o, sum[c], r, k);
+            Eight<T> e;
+            e.round(o);
+            e.store(dx + base + 8 * group, n);
+            if (db) {
+                if (d.dropped) drop8(d, offset, (uint32_t)group, (uint32_t)row, o);
+                e.round(o);
+                e.store(db + base + 8 * group, n);
+            }
+        }
+    }
+    if (!partial) return;
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+        const int at = 8 * (t + 64 * W * c), n = hidden - at;
+        Eight<float> e;
+        e.round(sum[c]);
+        if (n > 0) e.store(partial + (long)p * hidden + at, n);
+    }
+}
+
+// Rows too long for a workgroup's registers: asked for a second time, which the caches answer, and dg's sums in LDS (up to 128 KB).
+template <typename T>
+__global__ __launch_bounds__(1024) void k_add_norm_bwd_wide(Drop d, int rows, int hidden, int parts, float eps, const T* h, const T* __restrict__ g,
+                                                             const T* dxn, const T* dh, T* dx, T* db, float* __restrict__ partial) {
+    extern __shared__ __attribute__((aligned(16))) float sums[];   // a multiple of 8, each lane its own
+    __shared__ float red[2][2][16];
+    const int p = (int)blockIdx.x, chunks = (hidden + 7) / 8;
+    const uint64_t offset = db && d.dropped ? drop_offset(d) : 0;
+    for (int i = (int)threadIdx.x; i < chunks; i += 1024)
+#pragma unroll
+        for (int j = 0; j < 8; j++) sums[8 * i + j] = 0.f;
+    int turn = 0;
+    for (int row = p; row < rows; row += parts, turn ^= 1) {
+        const long base = (long)row * hidden;
+        float ss = 0.f, dot = 0.f;
+        for (int c = (int)threadIdx.x; c < chunks; c += 1024) {
+            const int at = 8 * c, n = hidden - at;
+            Eight<T> rh, ru, rg;
+            rh.load(h + base + at, n);
+            ru.load(dxn + base + at, n);
+            rg.load(g + at, n);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float a = rh.at(i);
+                ss = fmaf(a, a, ss);
+                dot = fmaf(ru.at(i) * rg.at(i), a, dot);
+            }
+        }
+        row_sums<16>(ss, dot, red[turn]);
+        const float r = 1.0f / sqrtf(ss / (float)hidden + eps), k = r * r * (dot / (float)hidden);
+        for (int c = (int)threadIdx.x; c < chunks; c += 1024) {
+            const int at = 8 * c, n = hidden - at;
+            Eight<T> e, rd{};
+            float a[8], u[8], w[8], o[8], sum[8];
+            e.load(h + base + at, n);
+            e.widen(a);
+            e.load(dxn + base + at, n);
+            e.widen(u);
+            e.load(g + at, n);
+            e.widen(w);
+            if (dh) rd.load(dh + base + at, n);
+            rd.widen(o);
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum[i] = sums[at + i];
+            norm_grad8(a, u, w, o, sum, r, k);
+#pragma unroll
+            for (int i = 0; i < 8; i++) sums[at + i] = sum[i];
+            e.round(o);
+            e.store(dx + base + at, n);
+            if (db) {
+                if (d.dropped) drop8(d, offset, (uint32_t)c, (uint32_t)row, o);
+                e.round(o);
+                e.store(db + base + at, n);
+            }
+        }
+    }
+    if (!partial) return;
+    for (int c = (int)threadIdx.x; c < chunks; c += 1024) {
+        Eight<float> e;
+        e.round(sums + 8 * c);
+        e.store(partial + (long)p * hidden + 8 * c, hidden - 8 * c);
+    }
+}
+
+// dg (+)= sum of the partial rows, in their order within each of four shares
+__global__ __launch_bounds__(256) void k_gain_sum(const float* __restrict__ partial, int parts, int hidden, float* dg, int accumulate) {
+    __shared__ float part[4][64];
+    const int share = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, col = (int)blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (col < hidden)
+        for (int p = share; p < parts; p += 4) s += partial[(long)p * hidden + col];
+    part[share][lane] = s;
+    __syncthreads();
+    if (share == 0 && col < hidden) {
+        s = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+        dg[col] = accumulate ? dg[col] + s : s;
+    }
+}
+
+int add_norm_partial_rows(int rows, int hidden) {
+    const int most = hidden <= 2048 ? 1024 : 512;
+    return rows < most ? rows : most;
+}
+
+template <typename T>
+static hipError_t bwd(const Drop& d, int rows, int hidden, float eps, const void* h, const void* g, const void* dxn, const void* dh, void* dx, void* db,
+                      float* partial, hipStream_t st) {
+    const int chunks = (hidden + 7) / 8, parts = add_norm_partial_rows(rows, hidden);
+    auto run = [&](auto kern, int each, int threads) {
+        kern<<<(parts + each - 1) / each, threads, 0, st>>>(d, rows, hidden, parts, eps, (const T*)h, (const T*)g, (const T*)dxn, (const T*)dh, (T*)dx,
+                                                            (T*)db, partial);
+        return hipGetLastError();
+    };
+#define HH_SHAPE(W, CH) if (chunks <= 64 * W * CH) return run(k_add_norm_bwd<T, W, CH>, rows_each<W>(), row_threads<W>())
+    HH_SHAPE(1, 1); HH_SHAPE(1, 2); HH_SHAPE(1, 4);
+    HH_SHAPE(8, 1); HH_SHAPE(8, 2); HH_SHAPE(8, 3);
+    if constexpr (sizeof(T) == 2) HH_SHAPE(8, 4);
+#undef HH_SHAPE
+    static std::atomic<uint64_t> lds_ok{0};
+    const int lds = chunks * 32;
+    const hipError_t e = allow_lds((const void*)&k_add_norm_bwd_wide<T>, 32768 * 4, lds_ok);
+    if (e != hipSuccess) return e;
+    k_add_norm_bwd_wide<T><<<parts, 1024, lds, st>>>(d, rows, hidden, parts, eps, (const T*)h, (const T*)g, (const T*)dxn, (const T*)dh, (T*)dx, (T*)db,
+                                                     partial);
+    return hipGetLastError();
+}
+hipError_t add_norm_bwd(int dtype, const Drop& d, int rows, int hidden, float eps, const void* h, const void* g, const void* dxn, const void* dh,
+                        void* dx, void* db, float* dg, int accumulate, float* partial, hipStream_t st) {
+    float* const to = dg ? partial : nullptr;
+    const hipError_t e = dtype == DT_BF16 ? bwd<bf16_t>(d, rows, hidden, eps, h, g, dxn, dh, dx, db, to, st)
+                                          : bwd<float>(d, rows, hidden, eps, h, g, dxn, dh, dx, db, to, st);
+    if (e != hipSuccess || !dg) return e;
+    k_gain_sum<<<(hidden + 63) / 64, 256, 0, st>>>(partial, add_norm_partial_rows(rows, hidden), hidden, dg, accumulate);
+    return hipGetLastError();
+}
+
+}  // namespace hh
