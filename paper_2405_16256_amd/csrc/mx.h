@@ -43,6 +43,30 @@ template <> struct Few<bf16_t, 8> {
         }
     }
 };
+template <> struct Few<bf16_t, 4> {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef u32x2 u32x2_any __attribute__((aligned(2)));
+    u32x2 w;
+    __device__ __forceinline__ void load(const bf16_t* p, int n) {
+        w = u32x2{0u, 0u};
+        if (n >= 4) w = *reinterpret_cast<const u32x2_any*>(p);
+        else {
+#pragma unroll
+            for (int i = 0; i < 3; i++)
+                if (i < n) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+        }
+    }
+    __device__ __forceinline__ float at(int i) const { return i & 1 ? hi_bf(w[i >> 1]) : lo_bf(w[i >> 1]); }
+    __device__ __forceinline__ void round(const float* f) { w = u32x2{pack_bf2(f[0], f[1]), pack_bf2(f[2], f[3])}; }
+    __device__ __forceinline__ void store(bf16_t* p, int n) const {
+        if (n >= 4) *reinterpret_cast<u32x2_any*>(p) = w;
+        else {
+#pragma unroll
+            for (int i = 0; i < 3; i++)
+                if (i < n) p[i] = (bf16_t)(w[i >> 1] >> (16 * (i & 1)));
+        }
+    }
+};
 template <int N> struct Few<float, N> {
     u32x4 w[N / 4];
     __device__ __forceinline__ void load(const float* p, int n) {
