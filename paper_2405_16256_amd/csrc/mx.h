@@ -16,6 +16,7 @@ __device__ __forceinline__ void store16(void* p, u32x4 v) { *reinterpret_cast<u3
 template <typename T, int N> struct Few;
 template <> struct Few<bf16_t, 8> {
     u32x4 w;
+    __device__ __forceinline__ void hide() { asm volatile("" : "+v"(w)); }   // the compiler forgets what it has derived from them
     __device__ __forceinline__ void load(const bf16_t* p, int n) {
         w = u32x4{0u, 0u, 0u, 0u};
         if (n >= 8) w = load16(p);
@@ -69,6 +70,7 @@ template <> struct Few<bf16_t, 4> {
 };
 template <int N> struct Few<float, N> {
     u32x4 w[N / 4];
+    __device__ __forceinline__ void hide() {}
     __device__ __forceinline__ void load(const float* p, int n) {
 #pragma unroll
         for (int q = 0; q < N / 4; q++) {

@@ -1,4 +1,6 @@
 // Dropout, and the residual's addition with its norm: forward and backward.  All of them stream their tensors once.
+#include <algorithm>
+
 #include "mx.h"
 
 namespace hh {
@@ -35,32 +37,42 @@ hipError_t dropout(int dtype, const Drop& d, long rows, long cols, const void* x
 template <int W> constexpr int row_threads() { return W == 1 ? 256 : 64 * W; }
 template <int W> constexpr int rows_each() { return W == 1 ? 4 : 1; }
 
-template <typename T, int W, int CH>
+// RAGGED: rows end inside a chunk.  The others are reached from a scalar address with a 32-bit distance, without a second path for the
+// last chunk: a third of the registers of a row of 12288.
+template <bool RAGGED> __device__ __forceinline__ int chunk_values(int hidden, int at) { return RAGGED ? hidden - at : at < hidden ? 8 : 0; }
+template <typename T> __device__ __forceinline__ T* chunk_at(T* row, int at) { return (T*)((char*)row + (uint32_t)at * (uint32_t)sizeof(T)); }
+template <typename T> __device__ __forceinline__ const T* chunk_at(const T* row, int at) { return (const T*)((const char*)row + (uint32_t)at * (uint32_t)sizeof(T)); }
+
+template <typename T, int W, int CH, bool RAGGED>
 __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int rows, int hidden, int width, float eps, const T* x, const T* b,
                                                                      const T* __restrict__ g, T* h, T* xn, int format, uint8_t* codes, uint8_t* scales) {
     __shared__ float red[W];
     const int t = (int)threadIdx.x & (64 * W - 1);
-    const int row = (int)blockIdx.x * rows_each<W>() + (W == 1 ? (int)threadIdx.x >> 6 : 0);
+    const int row = (int)blockIdx.x * rows_each<W>() + (W == 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0);
     if (row >= rows) return;   // one wave a row: no barrier follows
     const long base = (long)row * hidden;
+    const T* const x_row = x + base;
+    const T* const b_row = b + base;
+    T* const h_row = h + base;
+    T* const xn_row = xn + base;
     Eight<T> rx[CH], rb[CH], rg[CH];
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-        const int at = 8 * (t + 64 * W * c), n = hidden - at;
+        const int at = 8 * (t + 64 * W * c), n = chunk_values<RAGGED>(hidden, at);
         rx[c] = Eight<T>{};
         rb[c] = Eight<T>{};
         rg[c] = Eight<T>{};
         if (n > 0) {
-            rx[c].load(x + base + at, n);
-            if (b) rb[c].load(b + base + at, n);
-            rg[c].load(g + at, n);
+            rx[c].load(chunk_at(x_row, at), n);
+            if (b) rb[c].load(chunk_at(b_row, at), n);
+            rg[c].load(chunk_at(g, at), n);
         }
     }
     const uint64_t offset = b && d.dropped ? drop_offset(d) : 0;
     float v[CH][8], ss = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-        const int group = t + 64 * W * c, n = hidden - 8 * group;
+        const int group = t + 64 * W * c, n = chunk_values<RAGGED>(hidden, 8 * group);
         rx[c].widen(v[c]);
         if (b && n > 0) {
             float u[8];
@@ -69,7 +81,7 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
 #pragma unroll
             for (int i = 0; i < 8; i++) v[c][i] += u[i];
             rx[c].round(v[c]);
-            rx[c].store(h + base + 8 * group, n);
+            rx[c].store(chunk_at(h_row, 8 * group), n);
             rx[c].widen(v[c]);   // the norm is of the sum as it is kept
         }
 #pragma unroll
@@ -79,15 +91,15 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
     const float r = 1.0f / sqrtf(ss / (float)hidden + eps);
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-        const int group = t + 64 * W * c, n = hidden - 8 * group;
+        const int group = t + 64 * W * c, n = chunk_values<RAGGED>(hidden, 8 * group);
         float u[8];
         rg[c].widen(u);
 #pragma unroll
-        for (int i = 0; i < 8; i++) u[i] = i < n ? v[c][i] * r * u[i] : 0.f;
+        for (int i = 0; i < 8; i++) u[i] = i < n ? v[c][i] * r * u[i] : 0.f;   // past the end also where r is no number
         if (xn && n > 0) {
             Eight<T> e;
             e.round(u);
-            e.store(xn + base + 8 * group, n);
+            e.store(chunk_at(xn_row, 8 * group), n);
         }
         if (format != MX_NONE && 8 * group < width) {   // whole blocks of 32: the four lanes of one are here together
             const uint32_t m = quad_max(magnitude8(u));
@@ -115,7 +127,8 @@ static hipError_t fwd(const Drop& d, int rows, int hidden, float eps, const void
                                                            q.codes, q.scales);
         return hipGetLastError();
     };
-#define HH_SHAPE(W, CH) if (chunks <= 64 * W * CH) return run(k_add_norm_fwd<T, W, CH>, rows_each<W>(), row_threads<W>())
+#define HH_SHAPE(W, CH) \
+    if (chunks <= 64 * W * CH) return hidden % 8 ? run(k_add_norm_fwd<T, W, CH, true>, rows_each<W>(), row_threads<W>()) : run(k_add_norm_fwd<T, W, CH, false>, rows_each<W>(), row_threads<W>())
     HH_SHAPE(1, 1); HH_SHAPE(1, 2); HH_SHAPE(1, 4);
     HH_SHAPE(4, 2); HH_SHAPE(4, 3); HH_SHAPE(4, 4); HH_SHAPE(4, 6);
     HH_SHAPE(16, 2); HH_SHAPE(16, 4);
@@ -151,39 +164,47 @@ __device__ __forceinline__ void row_sums(float& ss, float& dot, float (&red)[2][
     }
 }
 
-// Workgroups (waves, where a wave takes a row) walk rows p, p + P, ... and keep their sums for dg in registers; partial[p] of P.
-template <typename T, int W, int CH>
-__global__ __launch_bounds__(row_threads<W>()) void k_add_norm_bwd(Drop d, int rows, int hidden, int parts, float eps, const T* h, const T* __restrict__ g,
-                                                                     const T* dxn, const T* dh, T* dx, T* db, float* __restrict__ partial) {
+// Workgroups walk rows p, p + parts, ... (four of them at once where a wave takes one) and keep their sums for dg in registers; partial[p].
+// Registers of bf16 rows are held to what leaves four waves on a SIMD: a row's loads wait for no one but themselves, and the other waves'
+// cover them.
+template <typename T, int CH> constexpr int grad_waves() { return sizeof(T) == 2 && CH <= 3 ? 4 : 2; }
+template <typename T, int W, int CH, bool RAGGED>
+__global__ __launch_bounds__(row_threads<W>(), (RAGGED ? 2 : grad_waves<T, CH>())) void k_add_norm_bwd(Drop d, int rows, int hidden, int parts, float eps, const T* h,
+                                                                                          const T* __restrict__ g, const T* dxn, const T* dh, T* dx, T* db,
+                                                                                          float* __restrict__ partial) {
     __shared__ float red[2][2][W];
-    const int t = (int)threadIdx.x & (64 * W - 1);
-    const int p = (int)blockIdx.x * rows_each<W>() + (W == 1 ? (int)threadIdx.x >> 6 : 0);
-    if (p >= parts) return;
+    const int t = (int)threadIdx.x & (64 * W - 1), sub = W == 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
+    const int p = (int)blockIdx.x;
     const uint64_t offset = db && d.dropped ? drop_offset(d) : 0;
     Eight<T> rg[CH];
     float sum[CH][8];
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-        const int at = 8 * (t + 64 * W * c), n = hidden - at;
+        const int at = 8 * (t + 64 * W * c), n = chunk_values<RAGGED>(hidden, at);
         rg[c] = Eight<T>{};
-        if (n > 0) rg[c].load(g + at, n);
+        if (n > 0) rg[c].load(chunk_at(g, at), n);
 #pragma unroll
         for (int i = 0; i < 8; i++) sum[c][i] = 0.f;
     }
     int turn = 0;
-    for (int row = p; row < rows; row += parts, turn ^= 1) {
+    for (int row = p * rows_each<W>() + sub; row < rows; row += parts * rows_each<W>(), turn ^= 1) {
         const long base = (long)row * hidden;
+        const T* const h_row = h + base;
+        const T* const dxn_row = dxn + base;
+        const T* const dh_row = dh + base;
+        T* const dx_row = dx + base;
+        T* const db_row = db + base;
         Eight<T> rh[CH], ru[CH], rd[CH];
 #pragma unroll
         for (int c = 0; c < CH; c++) {
-            const int at = 8 * (t + 64 * W * c), n = hidden - at;
+            const int at = 8 * (t + 64 * W * c), n = chunk_values<RAGGED>(hidden, at);
             rh[c] = Eight<T>{};
             ru[c] = Eight<T>{};
             rd[c] = Eight<T>{};
             if (n > 0) {
-                rh[c].load(h + base + at, n);
-                ru[c].load(dxn + base + at, n);
-                if (dh) rd[c].load(dh + base + at, n);
+                rh[c].load(chunk_at(h_row, at), n);
+                ru[c].load(chunk_at(dxn_row, at), n);
+                if (dh) rd[c].load(chunk_at(dh_row, at), n);
             }
         }
         float ss = 0.f, dot = 0.f;
@@ -200,7 +221,13 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_bwd(Drop d, int r
         const float r = 1.0f / sqrtf(ss / (float)hidden + eps), k = r * r * (dot / (float)hidden);
 #pragma unroll
         for (int c = 0; c < CH; c++) {
-            const int group = t + 64 * W * c, n = hidden - 8 * group;
+            __builtin_amdgcn_sched_barrier(0);   // a chunk at a time
+            rh[c].hide();                        // kept as they lie in memory, and widened a second time
+            ru[c].hide();
+            rg[c].hide();
+            int group = t + 64 * W * c;
+            asm("" : "+v"(group));   // what the generator makes of it is not kept from row to row
+            const int n = chunk_values<RAGGED>(hidden, 8 * group);
             if (n <= 0) continue;
             float a[8], u[8], w[8], o[8];
             rh[c].widen(a);
@@ -210,21 +237,37 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_bwd(Drop d, int r
             norm_grad8(a, u, w, o, sum[c], r, k);
             Eight<T> e;
             e.round(o);
-            e.store(dx + base + 8 * group, n);
+            e.store(chunk_at(dx_row, 8 * group), n);
             if (db) {
                 if (d.dropped) drop8(d, offset, (uint32_t)group, (uint32_t)row, o);
                 e.round(o);
-                e.store(db + base + 8 * group, n);
+                e.store(chunk_at(db_row, 8 * group), n);
             }
         }
     }
     if (!partial) return;
+    if constexpr (W == 1) {   // the four waves' sums as one
+        __shared__ __attribute__((aligned(16))) float part[3][512 * CH];
+        if (sub) {
+#pragma unroll
+            for (int c = 0; c < CH; c++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) part[sub - 1][8 * (t + 64 * c) + i] = sum[c][i];
+        }
+        __syncthreads();
+        if (sub) return;
+#pragma unroll
+        for (int c = 0; c < CH; c++)
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                sum[c][i] = (sum[c][i] + part[0][8 * (t + 64 * c) + i]) + (part[1][8 * (t + 64 * c) + i] + part[2][8 * (t + 64 * c) + i]);
+    }
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-        const int at = 8 * (t + 64 * W * c), n = hidden - at;
+        const int at = 8 * (t + 64 * W * c), n = chunk_values<RAGGED>(hidden, at);
         Eight<float> e;
         e.round(sum[c]);
-        if (n > 0) e.store(partial + (long)p * hidden + at, n);
+        if (n > 0) e.store(chunk_at(partial + (long)p * hidden, at), n);
     }
 }
 
@@ -292,38 +335,46 @@ __global__ __launch_bounds__(1024) void k_add_norm_bwd_wide(Drop d, int rows, in
     }
 }
 
-// dg (+)= sum of the partial rows, in their order within each of four shares
-__global__ __launch_bounds__(256) void k_gain_sum(const float* __restrict__ partial, int parts, int hidden, float* dg, int accumulate) {
-    __shared__ float part[4][64];
+// dg (+)= sum of the partial rows: 64 columns a workgroup, each of its 16 waves every sixteenth row, in a fixed order.
+__global__ __launch_bounds__(1024) void k_gain_sum(const float* __restrict__ partial, int parts, int hidden, float* dg, int accumulate) {
+    __shared__ float part[16][64];
     const int share = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, col = (int)blockIdx.x * 64 + lane;
     float s = 0.f;
-    if (col < hidden)
-        for (int p = share; p < parts; p += 4) s += partial[(long)p * hidden + col];
+    if (col < hidden) {
+        const float* at = partial + (long)share * hidden + col;
+        const long step = 16L * hidden;
+        int p = share;
+        for (; p + 48 < parts; p += 64, at += 4 * step) {
+            const float a = at[0], b = at[step], c = at[2 * step], d = at[3 * step];
+            s += (a + b) + (c + d);
+        }
+        for (; p < parts; p += 16, at += step) s += *at;
+    }
     part[share][lane] = s;
     __syncthreads();
     if (share == 0 && col < hidden) {
-        s = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i++) s += part[i][lane];
         dg[col] = accumulate ? dg[col] + s : s;
     }
 }
 
-int add_norm_partial_rows(int rows, int hidden) {
-    const int most = hidden <= 2048 ? 1024 : 512;
-    return rows < most ? rows : most;
-}
+// Workgroups: as many as the chip holds at once, with a row (four of them) each at least.
+int add_norm_partial_rows(int rows, int hidden) { return std::min(hidden <= 1024 ? (rows + 3) / 4 : rows, 512); }
 
 template <typename T>
 static hipError_t bwd(const Drop& d, int rows, int hidden, float eps, const void* h, const void* g, const void* dxn, const void* dh, void* dx, void* db,
                       float* partial, hipStream_t st) {
     const int chunks = (hidden + 7) / 8, parts = add_norm_partial_rows(rows, hidden);
-    auto run = [&](auto kern, int each, int threads) {
-        kern<<<(parts + each - 1) / each, threads, 0, st>>>(d, rows, hidden, parts, eps, (const T*)h, (const T*)g, (const T*)dxn, (const T*)dh, (T*)dx,
-                                                            (T*)db, partial);
+    auto run = [&](auto kern, int threads) {
+        kern<<<parts, threads, 0, st>>>(d, rows, hidden, parts, eps, (const T*)h, (const T*)g, (const T*)dxn, (const T*)dh, (T*)dx, (T*)db, partial);
         return hipGetLastError();
     };
-#define HH_SHAPE(W, CH) if (chunks <= 64 * W * CH) return run(k_add_norm_bwd<T, W, CH>, rows_each<W>(), row_threads<W>())
-    HH_SHAPE(1, 1); HH_SHAPE(1, 2); HH_SHAPE(1, 4);
-    HH_SHAPE(8, 1); HH_SHAPE(8, 2); HH_SHAPE(8, 3);
+#define HH_SHAPE(W, CH) \
+    if (chunks <= 64 * W * CH) return hidden % 8 ? run(k_add_norm_bwd<T, W, CH, true>, row_threads<W>()) : run(k_add_norm_bwd<T, W, CH, false>, row_threads<W>())
+    HH_SHAPE(1, 1); HH_SHAPE(1, 2);
+    HH_SHAPE(4, 1); HH_SHAPE(8, 1); HH_SHAPE(8, 2); HH_SHAPE(8, 3);
     if constexpr (sizeof(T) == 2) HH_SHAPE(8, 4);
 #undef HH_SHAPE
     static std::atomic<uint64_t> lds_ok{0};
@@ -340,7 +391,7 @@ hipError_t add_norm_bwd(int dtype, const Drop& d, int rows, int hidden, float ep
     const hipError_t e = dtype == DT_BF16 ? bwd<bf16_t>(d, rows, hidden, eps, h, g, dxn, dh, dx, db, to, st)
                                           : bwd<float>(d, rows, hidden, eps, h, g, dxn, dh, dx, db, to, st);
     if (e != hipSuccess || !dg) return e;
-    k_gain_sum<<<(hidden + 63) / 64, 256, 0, st>>>(partial, add_norm_partial_rows(rows, hidden), hidden, dg, accumulate);
+    k_gain_sum<<<(hidden + 63) / 64, 1024, 0, st>>>(partial, add_norm_partial_rows(rows, hidden), hidden, dg, accumulate);
     return hipGetLastError();
 }
 

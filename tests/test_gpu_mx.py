@@ -326,6 +326,23 @@ def test_add_norm_gradients(ctx, dtype, rows, hidden):
             within(np64(dg), dgw + base, (rows + 48) * E * (total + np.abs(base)), "dg")
 
 
+@pytest.mark.parametrize("hidden", (40, 257, 1003))
+def test_rows_that_are_no_numbers(ctx, hidden):
+    """A row with a NaN, and one of zeros without eps, are NaNs as far as they go and nothing behind; the other rows are as without them."""
+    x = torch.ones(4, hidden, dtype=torch.bfloat16, device=L.DEV)
+    x[1, 3] = float("nan")
+    x[2] = 0
+    g = torch.ones(hidden, dtype=torch.bfloat16, device=L.DEV)
+    xn, q = torch.empty_like(x), Packed(4, hidden, "e4m3")
+    hh.hh_add_norm_fwd(ctx, hh.make_add_norm_cfg(4, hidden, 0.0, hh.HH_BF16, hh.HH_MX_E4M3), None, x, None, g, None, xn, q.struct, L.stream_ptr())
+    bad = np.isnan(np64(xn))
+    assert bad[1:3].all() and (np64(xn)[[0, 3]] == 1).all()
+    codes, scales = q.host()
+    blocks = -(-hidden // 32)
+    assert (scales[1:3, :blocks] == 255).all() and (scales[1:3, blocks:] == 0).all() and (codes[1:3, 32 * blocks:] == 0).all()
+    assert (O.values(codes, scales, hidden, O.E4M3)[[0, 3]] == 1).all()
+
+
 def test_rows_behind_the_last_are_left_alone(ctx):
     """Tensors of 5 rows in larger buffers."""
     rng = np.random.default_rng(8)
