@@ -9,106 +9,131 @@ namespace hh {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// What one lane holds of 32 rows x 64 k of an operand: row lane % 32 and, with h = lane / 32, of E2M1 the codes k = 32 h .. 32 h + 31, of E4M3
-// the codes 16 h .. 16 h + 15 and 32 + 16 h .. 32 + 16 h + 15.  The scale of a lane is that of k = 32 h .. 32 h + 31 in both.
-template <int F> __device__ __forceinline__ i32x8 fragment(const uint8_t* row, int k, int h);
-template <> __device__ __forceinline__ i32x8 fragment<MX_E2M1>(const uint8_t* row, int k, int h) {
-    const i32x4 a = *reinterpret_cast<const i32x4*>(row + k / 2 + 16 * h);
-    return i32x8{a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-}
-template <> __device__ __forceinline__ i32x8 fragment<MX_E4M3>(const uint8_t* row, int k, int h) {
-    const i32x4 a = *reinterpret_cast<const i32x4*>(row + k + 16 * h), b = *reinterpret_cast<const i32x4*>(row + k + 32 + 16 * h);
-    return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-}
-template <int F> constexpr int FORMAT = F == MX_E4M3 ? 0 : 4;   // of the matrix instruction
-
-// Widened to bfloat16 with their scale, exactly: 16 codes of a block, which this lane holds of 32 rows x 64 k twice, k = 32 q + 16 h .. + 15.
-typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
-template <int F> __device__ __forceinline__ void widen16(const uint8_t* row, int k, int h, float scale, bf16x8& lo, bf16x8& hi);
-template <> __device__ __forceinline__ void widen16<MX_E4M3>(const uint8_t* row, int k, int h, float scale, bf16x8& lo, bf16x8& hi) {
-    const i32x4 codes = *reinterpret_cast<const i32x4*>(row + k + 16 * h);
-    bf16x2v p[8];
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[i], scale, false);
-        p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[i], scale, true);
-    }
-    lo = bf16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
-    hi = bf16x8{p[4][0], p[4][1], p[5][0], p[5][1], p[6][0], p[6][1], p[7][0], p[7][1]};
-}
-template <> __device__ __forceinline__ void widen16<MX_E2M1>(const uint8_t* row, int k, int h, float scale, bf16x8& lo, bf16x8& hi) {
-    const i32x2 codes = *reinterpret_cast<const i32x2*>(row + k / 2 + 8 * h);
-    bf16x2v p[8];
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        p[4 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)codes[i], scale, 0);
-        p[4 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)codes[i], scale, 1);
-        p[4 * i + 2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)codes[i], scale, 2);
-        p[4 * i + 3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)codes[i], scale, 3);
-    }
-    lo = bf16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
-    hi = bf16x8{p[4][0], p[4][1], p[5][0], p[5][1], p[6][0], p[6][1], p[7][0], p[7][1]};
-}
-
 // ------------------------------------------------------------------ few rows
-// A workgroup of 4 waves forms 32x32 of C, each wave a quarter of k, straight from memory.  WIDE: on the bfloat16 instruction.
-template <int FA, int FB, bool WIDE, typename TC>
-__global__ __launch_bounds__(256) void k_product(MxProduct p, int width, int tiles_n) {
-    __shared__ float part[3][64][17];
-    const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, h = lane >> 5, l = lane & 31;
-    const int m0 = ((int)blockIdx.x / tiles_n) * 32, n0 = ((int)blockIdx.x % tiles_n) * 32;
-    const size_t ra = min(m0 + l, p.M - 1), rb = min(n0 + l, p.N - 1);   // rows past the end: any, their results are dropped
-    const uint8_t* const a = p.a.codes + ra * (size_t)(FA == MX_E4M3 ? width : width / 2);
-    const uint8_t* const b = p.b.codes + rb * (size_t)(FB == MX_E4M3 ? width : width / 2);
-    const uint8_t* const sa = p.a.scales + ra * (size_t)(width / MX_BLOCK) + h;
-    const uint8_t* const sb = p.b.scales + rb * (size_t)(width / MX_BLOCK) + h;
-    f32x16 acc;
+// C of up to 16 TM rows: 16 columns a workgroup, its waves take 256 k at a time in turn, straight from memory into registers, and their sums
+// meet in LDS.  Bound by the one read of B: nothing of it is used twice, so it has no use for LDS, and what counts is that every wave of the
+// chip has its whole share under way at once.
+//
+// Of 16 rows x 128 k lane l holds row l % 16 and, with q = l / 16, of E2M1 the codes 32 q .. 32 q + 31, of E4M3 (and WIDE) 16 q .. 16 q + 15 and
+// 64 + 16 q .. 64 + 16 q + 15; its scale is that of k = 32 q .. 32 q + 31.
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+template <int F> __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale);   // 8 codes (E2M1: of lo) with their scale, exactly
+template <> __device__ __forceinline__ bf16x8 widen8<MX_E4M3>(uint32_t lo, uint32_t hi, float scale) {
+    const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2v c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+template <> __device__ __forceinline__ bf16x8 widen8<MX_E2M1>(uint32_t lo, uint32_t, float scale) {
+    const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(lo, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(lo, scale, 1);
+    const bf16x2v c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(lo, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(lo, scale, 3);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+template <int F, bool WIDE>
+struct RowUnit {   // 256 k of the lane's row
+    i32x4 v[F == MX_E4M3 ? 4 : 2];
+    uint2 s;
+    __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int unit, int q) {
+        if constexpr (F == MX_E4M3) {
 #pragma unroll
-    for (int i = 0; i < 16; i++) acc[i] = 0.f;
-    const int steps = (p.K + 63) / 64, from = steps * wave / 4, to = steps * (wave + 1) / 4;
-    for (int s = from; s < to; s++) {
-        if constexpr (WIDE) {
-            const uint8_t* const ba = sa - h + 2 * s;
-            const uint8_t* const bb = sb - h + 2 * s;
+            for (int i = 0; i < 4; i++) v[i] = *reinterpret_cast<const i32x4*>(codes + 256 * (long)unit + 64 * i + 16 * q);
+        } else if constexpr (WIDE) {
 #pragma unroll
-            for (int q = 0; q < 2; q++) {
-                bf16x8 a0, a1, b0, b1;
-                widen16<FA>(a, 64 * s + 32 * q, h, scale_value(ba[q]), a0, a1);
-                widen16<FB>(b, 64 * s + 32 * q, h, scale_value(bb[q]), b0, b1);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b0, a0, acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b1, a1, acc, 0, 0, 0);
+            for (int i = 0; i < 2; i++) {
+                const i32x2 a = *reinterpret_cast<const i32x2*>(codes + 128 * (long)unit + 64 * i + 8 * q);
+                const i32x2 b = *reinterpret_cast<const i32x2*>(codes + 128 * (long)unit + 64 * i + 32 + 8 * q);
+                v[i] = i32x4{a[0], a[1], b[0], b[1]};
             }
         } else {
-            const i32x8 fa = fragment<FA>(a, 64 * s, h), fb = fragment<FB>(b, 64 * s, h);
-            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb, fa, acc, FORMAT<FB>, FORMAT<FA>, 0, (int)sb[2 * s], 0, (int)sa[2 * s]);
+#pragma unroll
+            for (int i = 0; i < 2; i++) v[i] = *reinterpret_cast<const i32x4*>(codes + 128 * (long)unit + 64 * i + 16 * q);
+        }
+        s = *reinterpret_cast<const uint2*>(scales + 8 * (long)unit);
+    }
+    __device__ __forceinline__ i32x8 operand(int half) const {
+        if constexpr (F == MX_E4M3) {
+            const i32x4 a = v[2 * half], b = v[2 * half + 1];
+            return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        } else {
+            const i32x4 a = v[half];
+            return i32x8{a[0], a[1], a[2], a[3], 0, 0, 0, 0};
         }
     }
-    if (wave) {
-#pragma unroll
-        for (int i = 0; i < 16; i++) part[wave - 1][lane][i] = acc[i];
+    __device__ __forceinline__ int scale(int half, int q) const { return (int)((half ? s.y : s.x) >> (8 * q)); }
+    // 8 codes of the 16 at k = 128 half + 64 part + 16 q, widened
+    __device__ __forceinline__ bf16x8 widened(int half, int part, int eight, int q) const {
+        const float x = scale_value((half ? s.y : s.x) >> (16 * part + 8 * (q >> 1)) & 255u);
+        if constexpr (F == MX_E4M3) return widen8<F>((uint32_t)v[2 * half + part][2 * eight], (uint32_t)v[2 * half + part][2 * eight + 1], x);
+        else return widen8<F>((uint32_t)v[half][2 * part + eight], 0u, x);
     }
+};
+
+template <int F> constexpr int FORMAT = F == MX_E4M3 ? 0 : 4;   // of the matrix instruction
+struct MxRowsProblem { const uint8_t *a, *b, *sa, *sb; void* C; long ldc; int M, N, units, accumulate; uint32_t pitch_a, pitch_b, pitch_s; };
+
+template <int FA, int FB, bool WIDE, typename TC, int TM, int NW>
+__global__ __launch_bounds__(64 * NW) void k_product_rows(MxRowsProblem p) {
+    __shared__ float part[NW][TM][256];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
+    const int n0 = (int)blockIdx.x * 16;
+    const uint32_t rb = (uint32_t)min(n0 + l, p.N - 1);   // rows past the end: any, their results are dropped
+    const uint8_t* const b = p.b + (size_t)rb * p.pitch_b;
+    const uint8_t* const sb = p.sb + (size_t)rb * p.pitch_s;
+    const uint8_t *a[TM], *sa[TM];
+    f32x4 acc[TM];
+#pragma unroll
+    for (int i = 0; i < TM; i++) {
+        const uint32_t ra = (uint32_t)min(16 * i + l, p.M - 1);
+        a[i] = p.a + (size_t)ra * p.pitch_a;
+        sa[i] = p.sa + (size_t)ra * p.pitch_s;
+        acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll 4
+    for (int u = wave; u < p.units; u += NW) {
+        RowUnit<FB, WIDE> ub;
+        RowUnit<FA, WIDE> ua[TM];
+        ub.load(b, sb, u, q);
+#pragma unroll
+        for (int i = 0; i < TM; i++) ua[i].load(a[i], sa[i], u, q);
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    const bf16x8 w = ub.widened(half, x >> 1, x & 1, q);
+#pragma unroll
+                    for (int i = 0; i < TM; i++) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, ua[i].widened(half, x >> 1, x & 1, q), acc[i], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < TM; i++)
+                    acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ub.operand(half), ua[i].operand(half), acc[i], FORMAT<FB>, FORMAT<FA>, 0,
+                                                                            ub.scale(half, q), 0, ua[i].scale(half, q));
+            }
+        }
+    }
+    // a lane has row l of a block of C and columns 4 q .. 4 q + 3
+#pragma unroll
+    for (int i = 0; i < TM; i++) *reinterpret_cast<f32x4*>(&part[wave][i][16 * l + 4 * q]) = acc[i];
     __syncthreads();
-    if (wave) return;
+    for (int e = (int)threadIdx.x; e < 256 * TM; e += 64 * NW) {
+        const int m = e >> 4, n = n0 + (e & 15);
+        if (m >= p.M || n >= p.N) continue;
+        float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < 3; w++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) acc[i] += part[w][lane][i];
-    // a lane has row l of C and columns 8 q + 4 h .. + 3
-    const int m = m0 + l;
-    if (m >= p.M) return;
-    TC* const c = (TC*)p.C + (long)m * p.ldc;
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const int n = n0 + 8 * (i >> 2) + 4 * h + (i & 3);
-        if (n >= p.N) continue;
-        if constexpr (sizeof(TC) == 4) c[n] = p.accumulate ? c[n] + acc[i] : acc[i];
-        else c[n] = f2bf(p.accumulate ? bf2f(c[n]) + acc[i] : acc[i]);
+        for (int w = 0; w < NW; w++) v += part[w][e >> 8][e & 255];
+        if constexpr (sizeof(TC) == 4) {
+            float* const c = (float*)p.C + (long)m * p.ldc + n;
+            *c = p.accumulate ? *c + v : v;
+        } else {
+            bf16_t* const c = (bf16_t*)p.C + (long)m * p.ldc + n;
+            *c = f2bf(p.accumulate ? bf2f(*c) + v : v);
+        }
     }
 }
 
-
 // ------------------------------------------------------------------ tiles
-// BM x BN of C a workgroup, WR x WC waves, each 32 TM x 32 TN.  k advances KS at a time through two LDS stages that are filled straight from
+// BM x BN of C a workgroup, WR x WC waves, each 32 TM x 32 TN.  k advances KS at a time through NS LDS stages that are filled straight from
 // global memory; a row of a stage is 128 bytes of E4M3 (KS 128), or 64 beside that, or 128 of E2M1 on both sides (KS 256), and the scales of
 // those k lie behind the tiles.  16-byte chunks are XOR-swizzled by the row so that a fragment's 16 lanes cover all banks.
 template <int F, int KS> constexpr int ROW_BYTES = F == MX_E4M3 ? KS : KS / 2;
@@ -125,7 +150,8 @@ __device__ __forceinline__ i32x4 rsrc_words(const void* p, uint32_t bytes) {
     return i32x4{(int)(uint32_t)a, (int)(uint32_t)(a >> 32), (int)bytes, 0x00020000};
 }
 
-// One operand's share of a stage: its tile and its scales.
+// One operand's share of a stage: its tile and its scales.  Of 32 rows x 64 k lane l holds row l % 32 and, with h = l / 32, of E2M1 the codes
+// k = 32 h .. 32 h + 31, of E4M3 (and WIDE) 16 h .. 16 h + 15 and 32 + 16 h .. 32 + 16 h + 15; its scale is that of k = 32 h .. 32 h + 31.
 template <int F, int KS, int ROWS, int NW>
 struct MxTile {
     static constexpr int RB = ROW_BYTES<F, KS>, SB = KS / MX_BLOCK, BYTES = ROWS * RB, SCALES = ROWS * SB;
@@ -166,22 +192,8 @@ struct MxTile {
     }
     // piece 2 q + p: codes 8 p .. of the lane's 16 of block q
     __device__ static __forceinline__ bf16x8 widen_piece(const Frag& f, int piece, float scale) {
-        bf16x2v p[4];
-        if constexpr (F == MX_E4M3) {
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const uint32_t w = (uint32_t)f.v[piece >> 1][2 * (piece & 1) + i];
-                p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
-                p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true);
-            }
-        } else {
-            const uint32_t w = (uint32_t)f.v[0][piece];
-            p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
-            p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
-            p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
-            p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
-        }
-        return bf16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
+        if constexpr (F == MX_E4M3) return widen8<F>((uint32_t)f.v[piece >> 1][2 * (piece & 1)], (uint32_t)f.v[piece >> 1][2 * (piece & 1) + 1], scale);
+        else return widen8<F>((uint32_t)f.v[0][piece], 0u, scale);
     }
     // The scales of a stage for rows rb .. rb + 31: not WIDE, byte (KS 256: s, KS 128: 2 s) is that of step s for this lane's half; WIDE, bytes
     // 2 s and 2 s + 1 are those of step s.
@@ -213,14 +225,13 @@ struct MxProblem {
     TileMap map;
 };
 
-template <int FA, int FB, bool WIDE, typename TC, int BM, int BN, int WR, int WC>
+template <int FA, int FB, bool WIDE, typename TC, int BM, int BN, int WR, int WC, int NS>
 __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
     constexpr int KS = STAGE_K<FA, FB>, NW = WR * WC, TM = BM / WR / 32, TN = BN / WC / 32, STEPS = KS / 64, Q = STEPS * TM;
     using A = MxTile<FA, KS, BM, NW>;
     using B = MxTile<FB, KS, BN, NW>;
     constexpr int STAGE = A::BYTES + B::BYTES + A::SCALES + B::SCALES, AT_B = A::BYTES, AT_SA = AT_B + B::BYTES, AT_SB = AT_SA + A::SCALES;
-    constexpr int PARTS = A::PER_WAVE + B::PER_WAVE, SCALE_PARTS = (A::SCALE_PARTS + B::SCALE_PARTS) / NW;
-    static_assert(SCALE_PARTS * NW == A::SCALE_PARTS + B::SCALE_PARTS, "the scales split evenly over the waves");
+    constexpr int PARTS = A::PER_WAVE + B::PER_WAVE, SCALE_PARTS = (A::SCALE_PARTS + B::SCALE_PARTS + NW - 1) / NW;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
     const int wm = (wave / WC) * 32 * TM, wn = (wave % WC) * 32 * TN;
@@ -237,8 +248,8 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
 #pragma unroll
     for (int i = 0; i < B::PER_WAVE; i++) voB[i] = B::voff(wave, i, n0, p.pitch_b) + first * B::RB;
 #pragma unroll
-    for (int i = 0; i < SCALE_PARTS; i++) {   // of A, then of B
-        const int part = uwave + NW * i, of_b = part - A::SCALE_PARTS;
+    for (int i = 0; i < SCALE_PARTS; i++) {   // of A, then of B; where there are fewer than waves, some fetch the same
+        const int part = (uwave + NW * i) % (A::SCALE_PARTS + B::SCALE_PARTS), of_b = part - A::SCALE_PARTS;
         rsS[i] = of_b < 0 ? rsrc_words(p.sa, p.sa_bytes) : rsrc_words(p.sb, p.sb_bytes);
         toS[i] = of_b < 0 ? AT_SA + part * 256 : AT_SB + of_b * 256;
         voS[i] = (of_b < 0 ? A::scale_voff(part, m0, p.pitch_s) : B::scale_voff(of_b, n0, p.pitch_s)) + first * A::SB;
@@ -265,17 +276,28 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
         for (int j = 0; j < TN; j++)
 #pragma unroll
             for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
+    // Behind the last stage nothing is there to be fetched.  The requests go out all the same, to buffers of no extent: with a branch around
+    // them the compiler moves the matrix instructions in front of it behind it.
+    auto past_the_end = [&](bool past) {
+        if (past) {
+            rsA[2] = rsB[2] = 0;
 #pragma unroll
-    for (int s = 0; s < 2; s++)
-        if (s < nk) {
-#pragma unroll
-            for (int i = 0; i < ALL; i++) dma_part(s, i);
+            for (int x = 0; x < SCALE_PARTS; x++) rsS[x][2] = 0;
         }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+#pragma unroll
+    for (int s = 0; s < NS; s++) {
+        past_the_end(s >= nk);
+#pragma unroll
+        for (int i = 0; i < ALL; i++) dma_part(s, i);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * ALL) : "memory");
     __syncthreads();
 
     // Fragments of A are fetched AHEAD of their products, those of B a step ahead; scales with the first fragments of their stage.
-    constexpr int AHEAD = 3, RING = 4;
+    // AHEAD is at most TM: the last fragments of B that a stage has are asked for in its last step but one, which has to be before the barrier.
+    constexpr int AHEAD = TM >= 4 ? 3 : TM, RING = AHEAD == 1 ? 2 : 4;
+    static_assert(AHEAD <= TM && AHEAD < RING, "see above");
     static_assert(Q % RING == 0 && STEPS % 2 == 0, "a stage ends where it began in both rings");
     typename A::Frag fa[RING];
     typename B::Frag fb[2][TN];
@@ -288,23 +310,19 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
     for (int i = 0; i < TM; i++) sa[i] = A::template scales<WIDE>(smem + AT_SA, wm + 32 * i);
 #pragma unroll
     for (int j = 0; j < TN; j++) sb[j] = B::template scales<WIDE>(smem + AT_SB, wn + 32 * j);
+    int slot = 0;
     for (int kt = 0; kt < nk; kt++) {
-        const char* const cur = smem + (kt & 1) * STAGE;
-        const char* const nxt = smem + ((kt + 1) & 1) * STAGE;
-        // Behind the last stage nothing is there to be fetched.  The requests go out all the same, to buffers of no extent: with a branch around
-        // them the compiler moves the matrix instructions in front of it behind it.
-        if (kt + 2 >= nk) {
-            rsA[2] = rsB[2] = 0;
-#pragma unroll
-            for (int x = 0; x < SCALE_PARTS; x++) rsS[x][2] = 0;
-        }
+        const int next = slot + 1 == NS ? 0 : slot + 1;
+        const char* const cur = smem + slot * STAGE;
+        const char* const nxt = smem + next * STAGE;
+        past_the_end(kt + NS >= nk);
 #pragma unroll
         for (int q = 0; q < Q; q++) {
             const int step = q / TM, i = q % TM;
             __builtin_amdgcn_sched_barrier(0);
             if (q == Q - AHEAD) {
                 // Every wave has its last fragments of this stage, and the next stage has landed for all of them.
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * ALL) : "memory");
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
                 __builtin_amdgcn_sched_barrier(0);
@@ -323,7 +341,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
             if (q >= Q - AHEAD) {
 #pragma unroll
                 for (int x = 0; x < ALL; x++)
-                    if (x * AHEAD / ALL == q - (Q - AHEAD)) dma_part(kt & 1, x);
+                    if (x * AHEAD / ALL == q - (Q - AHEAD)) dma_part(slot, x);
             }
 #pragma unroll
             for (int j = 0; j < TN; j++) {
@@ -350,6 +368,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
         for (int x = 0; x < TM; x++) sa[x] = na[x];
 #pragma unroll
         for (int x = 0; x < TN; x++) sb[x] = nb[x];
+        slot = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();   // the stages are free for the way out
@@ -403,14 +422,70 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
         }
 }
 
-template <int FA, int FB, bool WIDE, typename TC, int BM, int BN, int WR, int WC>
-static hipError_t launch_tiles(const MxProduct& q, hipStream_t st) {
+// C (+)= sum of the shares of k, in their order
+template <typename TC>
+__global__ __launch_bounds__(256) void k_sum_shares(const float* __restrict__ partial, int shares, int groups, Divisor per_row, int M, int N, TC* C, long ldc,
+                                                     int accumulate) {
+    const int i = (int)(blockIdx.x * 256u + threadIdx.x);
+    if (i >= groups) return;
+    int row = i;
+    const int col = 4 * split_off(row, per_row), n = N - col;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < shares; s++) {
+        Few<float, 4> e;
+        e.load(partial + ((long)s * M + row) * N + col, n);
+#pragma unroll
+        for (int x = 0; x < 4; x++) v[x] += e.at(x);
+    }
+    TC* const c = C + row * ldc + col;
+    Few<TC, 4> e;
+    if (accumulate) {
+        e.load(c, n);
+#pragma unroll
+        for (int x = 0; x < 4; x++) v[x] += e.at(x);
+    }
+    e.round(v);
+    e.store(c, n);
+}
+
+// Which kernel takes a product, and how many shares of k: the least predicted time.  A workgroup of tiles takes ENDS_US to start and to write
+// its tile and STAGE_US a stage, the same alone on its compute unit as beside another one; shares cost a second launch and the traffic of
+// their sums.  Measured against the best of all plans at 39 shapes and formats of 64 to 4096 rows the choice is
+// within 8 %; 1003x700x2050, E4M3 by E2M1: tiles of 64 6.8 us, of 128 11.3, of 256 24; 2048x4096x4096 65, 44, 48; 4096x4096x4096 118, 85, 61.
+enum { ROWS_16, ROWS_32, TILES_64, TILES_128, TILES_256 };
+struct MxPlan { int kernel, split; };
+constexpr int CUS = 256;
+static MxPlan plan(const MxProduct& p) {
+    if (p.M <= 16) return {ROWS_16, 1};
+    if (p.M <= 32) return {ROWS_32, 1};
+    const bool four = p.fa == MX_E2M1 && p.fb == MX_E2M1;
+    constexpr float STAGE_US[3][3] = {{0.33f, 0.82f, 2.2f}, {0.26f, 0.65f, 1.85f}, {0.58f, 1.1f, 3.4f}};   // E2M1 (256 k), E4M3 (128 k), widened (128 k)
+    constexpr float ENDS_US[3] = {0.7f, 2.2f, 3.5f};
+    const float* const us = STAGE_US[four ? 0 : p.f32 ? 2 : 1];
+    const int stages = (p.K + (four ? 255 : 127)) / (four ? 256 : 128);
+    MxPlan best{TILES_64, 1};
+    float least = 0.f;
+    for (int i = 0; i < 3; i++) {
+        const int b = 64 << i;
+        const long tiles = (long)((p.M + b - 1) / b) * ((p.N + b - 1) / b);
+        for (int split = 1; split <= 16 && (split == 1 || (stages >= 2 * split && tiles * split <= 2 * CUS)); split *= 2) {
+            const long rounds = (tiles * split + CUS - 1) / CUS;
+            float t = 2.f + (float)rounds * (ENDS_US[i] + (float)((stages + split - 1) / split) * us[i]);
+            if (split > 1) t += 2.5f + (float)p.M * (float)p.N * (float)(4 * (split + 1)) / 2e6f;
+            if (least == 0.f || t < least) { least = t; best = {TILES_64 + i, split}; }
+        }
+    }
+    return best;
+}
+
+template <int FA, int FB, bool WIDE, typename TC, int BM, int BN, int WR, int WC, int NS>
+static hipError_t launch_tiles(const MxProduct& q, int split, void* ws, hipStream_t st) {
     constexpr int KS = STAGE_K<FA, FB>, NW = WR * WC;
     using A = MxTile<FA, KS, BM, NW>;
     using B = MxTile<FB, KS, BN, NW>;
-    constexpr int LDS = std::max(2 * (A::BYTES + B::BYTES + A::SCALES + B::SCALES), NW * 4096);
+    constexpr int LDS = std::max(NS * (A::BYTES + B::BYTES + A::SCALES + B::SCALES), NW * 4096);
     static std::atomic<uint64_t> lds_ok{0};
-    auto kern = &k_product_tiles<FA, FB, WIDE, TC, BM, BN, WR, WC>;
+    auto kern = &k_product_tiles<FA, FB, WIDE, TC, BM, BN, WR, WC, NS>;
     const hipError_t e = allow_lds((const void*)kern, LDS, lds_ok);
     if (e != hipSuccess) return e;
     const long width = mx_width(q.K);
@@ -422,42 +497,53 @@ static hipError_t launch_tiles(const MxProduct& q, hipStream_t st) {
     p.sa_bytes = (uint32_t)q.M * p.pitch_s; p.sb_bytes = (uint32_t)q.N * p.pitch_s;
     p.C = q.C; p.ldc = q.ldc; p.M = q.M; p.N = q.N; p.accumulate = q.accumulate;
     p.stages = (q.K + KS - 1) / KS;
-    p.split = 1;
+    p.split = split;
+    p.partial = (float*)ws;
     p.map = tile_map(q.M, q.N, BM, BN);
-    kern<<<p.map.tiles(), 64 * NW, LDS, st>>>(p);
+    kern<<<dim3(p.map.tiles(), split), 64 * NW, LDS, st>>>(p);
+    if (split > 1) {
+        const int per_row = (q.N + 3) / 4, groups = q.M * per_row;
+        k_sum_shares<TC><<<(groups + 255) / 256, 256, 0, st>>>(p.partial, split, groups, divisor(per_row), q.M, q.N, (TC*)q.C, q.ldc, q.accumulate);
+    }
+    return hipGetLastError();
+}
+template <int FA, int FB, bool WIDE, typename TC, int TM>
+static hipError_t launch_rows(const MxProduct& q, hipStream_t st) {
+    const long width = mx_width(q.K);
+    const MxRowsProblem p{q.a.codes, q.b.codes, q.a.scales, q.b.scales, q.C, q.ldc, q.M, q.N, (int)(width / 256), q.accumulate,
+                          (uint32_t)(FA == MX_E4M3 ? width : width / 2), (uint32_t)(FB == MX_E4M3 ? width : width / 2), (uint32_t)(width / MX_BLOCK)};
+    const int grid = (q.N + 15) / 16;
+    if (p.units <= 4) k_product_rows<FA, FB, WIDE, TC, TM, 4><<<grid, 256, 0, st>>>(p);
+    else if (p.units <= 8) k_product_rows<FA, FB, WIDE, TC, TM, 8><<<grid, 512, 0, st>>>(p);
+    else k_product_rows<FA, FB, WIDE, TC, TM, 16><<<grid, 1024, 0, st>>>(p);
     return hipGetLastError();
 }
 
-size_t mx_product_workspace(const MxProduct&) { return 0; }
+size_t mx_product_workspace(const MxProduct& p) {
+    const MxPlan l = plan(p);
+    return l.split > 1 ? (size_t)l.split * p.M * p.N * sizeof(float) : 0;
+}
 
-hipError_t mx_product(const MxProduct& p, void*, hipStream_t st) {
-    if ((long)p.M * p.N >= 256 * 256) {
-        auto tiles = [&](auto fa, auto fb) {
-            constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value;
-            constexpr bool WIDE = FA == MX_E4M3 || FB == MX_E4M3;
-            return p.f32 ? launch_tiles<FA, FB, WIDE, float, 256, 256, 2, 4>(p, st) : launch_tiles<FA, FB, false, bf16_t, 256, 256, 2, 4>(p, st);
-        };
-        std::integral_constant<int, MX_E4M3> e8;
-        std::integral_constant<int, MX_E2M1> e4;
-        return p.fa == MX_E4M3 ? (p.fb == MX_E4M3 ? tiles(e8, e8) : tiles(e8, e4)) : (p.fb == MX_E4M3 ? tiles(e4, e8) : tiles(e4, e4));
+template <int FA, int FB, bool WIDE, typename TC>
+static hipError_t run_product(const MxProduct& p, void* ws, hipStream_t st) {
+    const MxPlan l = plan(p);
+    switch (l.kernel) {
+        case ROWS_16: return launch_rows<FA, FB, WIDE, TC, 1>(p, st);
+        case ROWS_32: return launch_rows<FA, FB, WIDE, TC, 2>(p, st);
+        case TILES_64: return launch_tiles<FA, FB, WIDE, TC, 64, 64, 2, 2, 4>(p, l.split, ws, st);
+        case TILES_128: return launch_tiles<FA, FB, WIDE, TC, 128, 128, 2, 2, 2>(p, l.split, ws, st);
+        default: return launch_tiles<FA, FB, WIDE, TC, 256, 256, 2, 4, 2>(p, l.split, ws, st);
     }
-    const int width = (int)mx_width(p.K), tiles_n = (p.N + 31) / 32;
-    const unsigned grid = (unsigned)(((p.M + 31) / 32) * (long)tiles_n);
-    auto run = [&](auto kern) {
-        kern<<<grid, 256, 0, st>>>(p, width, tiles_n);
-        return hipGetLastError();
+}
+hipError_t mx_product(const MxProduct& p, void* ws, hipStream_t st) {
+    auto run = [&](auto fa, auto fb) {
+        constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value;
+        constexpr bool WIDE = FA == MX_E4M3 || FB == MX_E4M3;
+        return p.f32 ? run_product<FA, FB, WIDE, float>(p, ws, st) : run_product<FA, FB, false, bf16_t>(p, ws, st);
     };
-    const bool a8 = p.fa == MX_E4M3, b8 = p.fb == MX_E4M3;
-    if (p.f32) {
-        if (a8 && b8) return run(k_product<MX_E4M3, MX_E4M3, true, float>);
-        if (a8) return run(k_product<MX_E4M3, MX_E2M1, true, float>);
-        if (b8) return run(k_product<MX_E2M1, MX_E4M3, true, float>);
-        return run(k_product<MX_E2M1, MX_E2M1, false, float>);
-    }
-    if (a8 && b8) return run(k_product<MX_E4M3, MX_E4M3, false, bf16_t>);
-    if (a8) return run(k_product<MX_E4M3, MX_E2M1, false, bf16_t>);
-    if (b8) return run(k_product<MX_E2M1, MX_E4M3, false, bf16_t>);
-    return run(k_product<MX_E2M1, MX_E2M1, false, bf16_t>);
+    std::integral_constant<int, MX_E4M3> e8;
+    std::integral_constant<int, MX_E2M1> e4;
+    return p.fa == MX_E4M3 ? (p.fb == MX_E4M3 ? run(e8, e8) : run(e8, e4)) : (p.fb == MX_E4M3 ? run(e4, e8) : run(e4, e4));
 }
 
 }  // namespace hh
