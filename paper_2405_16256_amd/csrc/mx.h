@@ -48,6 +48,7 @@ template <> struct Few<bf16_t, 4> {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     typedef u32x2 u32x2_any __attribute__((aligned(2)));
     u32x2 w;
+    __device__ __forceinline__ void hide() { asm volatile("" : "+v"(w)); }
     __device__ __forceinline__ void load(const bf16_t* p, int n) {
         w = u32x2{0u, 0u};
         if (n >= 4) w = *reinterpret_cast<const u32x2_any*>(p);
@@ -70,7 +71,10 @@ template <> struct Few<bf16_t, 4> {
 };
 template <int N> struct Few<float, N> {
     u32x4 w[N / 4];
-    __device__ __forceinline__ void hide() {}
+    __device__ __forceinline__ void hide() {
+#pragma unroll
+        for (int i = 0; i < N / 4; i++) asm volatile("" : "+v"(w[i]));
+    }
     __device__ __forceinline__ void load(const float* p, int n) {
 #pragma unroll
         for (int q = 0; q < N / 4; q++) {
