@@ -1,11 +1,13 @@
 // Packing to microscaled formats and back.
+#include <type_traits>
+
 #include "mx.h"
 
 namespace hh {
 
 // ------------------------------------------------------------------ by row
 // Eight values a lane, four lanes a block.
-template <typename T, int F>
+template <typename T, int F, bool STREAM>
 __global__ __launch_bounds__(256) void k_pack_rows(int chunks, Divisor per_row, int cols, const T* __restrict__ x, long ldx, uint8_t* __restrict__ codes,
                                                     uint8_t* __restrict__ scales) {
     const int i = (int)(blockIdx.x * 256u + threadIdx.x);
@@ -13,7 +15,7 @@ __global__ __launch_bounds__(256) void k_pack_rows(int chunks, Divisor per_row, 
     int row = i;
     const int group = split_off(row, per_row), n = cols - 8 * group;
     Eight<T> e{};
-    if (n > 0) e.load(x + row * ldx + 8L * group, n);
+    if (n > 0) e.template load<STREAM>(x + row * ldx + 8L * group, n);
     float v[8];
     e.widen(v);
     const uint32_t byte = scale_byte<F>(quad_max(magnitude8(v)));
@@ -59,7 +61,7 @@ template <> struct Magnitudes<float> {
 // ------------------------------------------------------------------ by column, and both
 // A lane takes 4 columns of a block of 32 rows in registers, ACROSS lanes the columns beside them and 64 / ACROSS the row blocks below: blocks
 // along columns need no exchange at all, those along rows one of eight lanes, and x is read once for both.
-template <typename T, int F, bool ROWS, int ACROSS>
+template <typename T, int F, bool ROWS, int ACROSS, bool STREAM>
 __global__ __launch_bounds__(256) void k_pack_columns(long rows, int cols, const T* __restrict__ x, long ldx, int width, uint8_t* __restrict__ codes,
                                                        uint8_t* __restrict__ scales, long column_width, uint8_t* __restrict__ column_codes,
                                                        uint8_t* __restrict__ column_scales, Divisor tiles_across) {
@@ -74,12 +76,12 @@ __global__ __launch_bounds__(256) void k_pack_columns(long rows, int cols, const
     Few<T, 4> raw[32];
     if (__all(n >= 4 && there == 32)) {
 #pragma unroll
-        for (int r = 0; r < 32; r++) raw[r].load(from + r * ldx, 4);
+        for (int r = 0; r < 32; r++) raw[r].template load<STREAM>(from + r * ldx, 4);
     } else {
 #pragma unroll
         for (int r = 0; r < 32; r++) {
             raw[r] = Few<T, 4>{};
-            if (n > 0 && r < there) raw[r].load(from + r * ldx, n);
+            if (n > 0 && r < there) raw[r].template load<STREAM>(from + r * ldx, n);
         }
     }
     Magnitudes<T> most(raw[0]);
@@ -134,17 +136,19 @@ __global__ __launch_bounds__(256) void k_pack_columns(long rows, int cols, const
 template <typename T, int F>
 static hipError_t quantise(long rows, long cols, const void* x, long ldx, const MxRows& by_row, const MxRows& by_column, hipStream_t st) {
     const int width = (int)mx_width(cols);
+    const bool stream = (double)rows * cols * (sizeof(T) + (F == MX_E4M3 ? 1.0 : 0.5) * ((by_row.codes != nullptr) + (by_column.codes != nullptr))) > STREAM_BYTES;
     if (!by_column.codes) {
         const int chunks = (int)(rows * (width / 8));
-        k_pack_rows<T, F><<<((unsigned)chunks + 255u) / 256u, 256, 0, st>>>(chunks, divisor(width / 8), (int)cols, (const T*)x, ldx, by_row.codes,
-                                                                           by_row.scales);
+        auto kern = stream ? &k_pack_rows<T, F, true> : &k_pack_rows<T, F, false>;
+        kern<<<((unsigned)chunks + 255u) / 256u, 256, 0, st>>>(chunks, divisor(width / 8), (int)cols, (const T*)x, ldx, by_row.codes, by_row.scales);
         return hipGetLastError();
     }
     const long column_width = mx_width(rows);
     constexpr int ACROSS = 16;   // 8 and 32 lanes: 34.3 and 31.9 us where 16 take 32.0, and as much by column alone
     const int across = ((by_row.codes ? width : (int)cols) + 16 * ACROSS - 1) / (16 * ACROSS);
     const unsigned grid = (unsigned)(across * ((column_width + 2048 / ACROSS - 1) / (2048 / ACROSS)));
-    auto kern = by_row.codes ? &k_pack_columns<T, F, true, ACROSS> : &k_pack_columns<T, F, false, ACROSS>;
+    auto kern = by_row.codes ? (stream ? &k_pack_columns<T, F, true, ACROSS, true> : &k_pack_columns<T, F, true, ACROSS, false>)
+                             : (stream ? &k_pack_columns<T, F, false, ACROSS, true> : &k_pack_columns<T, F, false, ACROSS, false>);
     kern<<<grid, 256, 0, st>>>(rows, (int)cols, (const T*)x, ldx, width, by_row.codes, by_row.scales, column_width, by_column.codes, by_column.scales,
                                divisor(across));
     return hipGetLastError();
@@ -159,7 +163,7 @@ hipError_t mx_quantise(int dtype, long rows, long cols, const void* x, long ldx,
 }
 
 // ------------------------------------------------------------------ values
-template <typename T, int F>
+template <typename T, int F, bool STREAM>
 __global__ __launch_bounds__(256) void k_values(int chunks, Divisor per_row, int k, int width, const uint8_t* __restrict__ codes,
                                                  const uint8_t* __restrict__ scales, T* __restrict__ y, long ldy) {
     const int i = (int)(blockIdx.x * 256u + threadIdx.x);
@@ -187,7 +191,7 @@ __global__ __launch_bounds__(256) void k_values(int chunks, Divisor per_row, int
     for (int j = 0; j < 8; j++) v[j] *= s;
     Eight<T> e;
     e.round(v);
-    e.store(y + row * ldy + 8L * group, k - 8 * group);
+    e.template store<STREAM>(y + row * ldy + 8L * group, k - 8 * group);
 }
 
 hipError_t mx_values(int dtype, long rows, long k, int format, const MxRows& q, void* y, long ldy, hipStream_t st) {
@@ -197,8 +201,16 @@ hipError_t mx_values(int dtype, long rows, long k, int format, const MxRows& q, 
         kern<<<grid, 256, 0, st>>>(chunks, divisor(per_row), (int)k, width, q.codes, q.scales, to, ldy);
         return hipGetLastError();
     };
-    if (dtype == DT_BF16) return format == MX_E4M3 ? run(k_values<bf16_t, MX_E4M3>, (bf16_t*)y) : run(k_values<bf16_t, MX_E2M1>, (bf16_t*)y);
-    return format == MX_E4M3 ? run(k_values<float, MX_E4M3>, (float*)y) : run(k_values<float, MX_E2M1>, (float*)y);
+    const bool stream = (double)rows * k * (dt_size(dtype) + (format == MX_E4M3 ? 1.0 : 0.5)) > STREAM_BYTES;
+    auto pick = [&](auto* to, auto fmt) {
+        typedef std::remove_pointer_t<decltype(to)> T;
+        constexpr int F = decltype(fmt)::value;
+        return run(stream ? &k_values<T, F, true> : &k_values<T, F, false>, to);
+    };
+    std::integral_constant<int, MX_E4M3> e8;
+    std::integral_constant<int, MX_E2M1> e4;
+    if (dtype == DT_BF16) return format == MX_E4M3 ? pick((bf16_t*)y, e8) : pick((bf16_t*)y, e4);
+    return format == MX_E4M3 ? pick((float*)y, e8) : pick((float*)y, e4);
 }
 
 }  // namespace hh

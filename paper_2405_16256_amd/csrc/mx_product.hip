@@ -195,17 +195,25 @@ struct MxTile {
         if constexpr (F == MX_E4M3) return widen8<F>((uint32_t)f.v[piece >> 1][2 * (piece & 1)], (uint32_t)f.v[piece >> 1][2 * (piece & 1) + 1], scale);
         else return widen8<F>((uint32_t)f.v[0][piece], 0u, scale);
     }
-    // The scales of a stage for rows rb .. rb + 31: not WIDE, byte (KS 256: s, KS 128: 2 s) is that of step s for this lane's half; WIDE, bytes
-    // 2 s and 2 s + 1 are those of step s.
-    template <bool WIDE> __device__ static __forceinline__ int scales(const char* lds, int rb) {
-        const int l = threadIdx.x & 63, r = rb + (l & 31), h = l >> 5;
+    // The scales of a stage for rows rb .. rb + 31, as they lie in LDS, and what the products take: not WIDE, byte (KS 256: s, KS 128: 2 s) is
+    // that of step s for this lane's half; WIDE, bytes 2 s and 2 s + 1 are those of step s.
+    struct Scales { uint32_t w[SB / 4]; };
+    __device__ static __forceinline__ Scales scales(const char* lds, int rb) {
+        const int r = rb + (int)(threadIdx.x & 31);
+        Scales s;
         if constexpr (SB == 8) {
             const uint2 w = *reinterpret_cast<const uint2*>(lds + 8 * r);
-            return (int)__builtin_amdgcn_perm(w.y, w.x, h ? 0x07050301u : 0x06040200u);
+            s.w[0] = w.x;
+            s.w[1] = w.y;
         } else {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(lds + 4 * r);
-            return (int)(WIDE ? w : w >> (8 * h));
+            s.w[0] = *reinterpret_cast<const uint32_t*>(lds + 4 * r);
         }
+        return s;
+    }
+    template <bool WIDE> __device__ static __forceinline__ int ordered(const Scales& s) {
+        const int h = (int)(threadIdx.x & 63) >> 5;
+        if constexpr (SB == 8) return (int)__builtin_amdgcn_perm(s.w[1], s.w[0], h ? 0x07050301u : 0x06040200u);
+        else return (int)(WIDE ? s.w[0] : s.w[0] >> (8 * h));
     }
 };
 
@@ -301,15 +309,17 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
     static_assert(Q % RING == 0 && STEPS % 2 == 0, "a stage ends where it began in both rings");
     typename A::Frag fa[RING];
     typename B::Frag fb[2][TN];
-    int sa[TM], sb[TN], na[TM], nb[TN];
+    int sa[TM], sb[TN];
+    typename A::Scales na[TM];
+    typename B::Scales nb[TN];
 #pragma unroll
     for (int q = 0; q < AHEAD; q++) fa[q] = A::template frag<WIDE>(smem, wm + 32 * (q % TM), q / TM);
 #pragma unroll
     for (int j = 0; j < TN; j++) fb[0][j] = B::template frag<WIDE>(smem + AT_B, wn + 32 * j, 0);
 #pragma unroll
-    for (int i = 0; i < TM; i++) sa[i] = A::template scales<WIDE>(smem + AT_SA, wm + 32 * i);
+    for (int i = 0; i < TM; i++) sa[i] = A::template ordered<WIDE>(A::scales(smem + AT_SA, wm + 32 * i));
 #pragma unroll
-    for (int j = 0; j < TN; j++) sb[j] = B::template scales<WIDE>(smem + AT_SB, wn + 32 * j);
+    for (int j = 0; j < TN; j++) sb[j] = B::template ordered<WIDE>(B::scales(smem + AT_SB, wn + 32 * j));
     int slot = 0;
     for (int kt = 0; kt < nk; kt++) {
         const int next = slot + 1 == NS ? 0 : slot + 1;
@@ -327,9 +337,9 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
                 asm volatile("" ::: "memory");
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < TM; x++) na[x] = A::template scales<WIDE>(nxt + AT_SA, wm + 32 * x);
+                for (int x = 0; x < TM; x++) na[x] = A::scales(nxt + AT_SA, wm + 32 * x);
 #pragma unroll
-                for (int x = 0; x < TN; x++) nb[x] = B::template scales<WIDE>(nxt + AT_SB, wn + 32 * x);
+                for (int x = 0; x < TN; x++) nb[x] = B::scales(nxt + AT_SB, wn + 32 * x);
             }
             const int f = q + AHEAD;
             fa[f % RING] = f < Q ? A::template frag<WIDE>(cur, wm + 32 * (f % TM), f / TM) : A::template frag<WIDE>(nxt, wm + 32 * (f % TM), f / TM - STEPS);
@@ -364,10 +374,11 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
                 }
             }
         }
+        __builtin_amdgcn_sched_barrier(0);   // the scales have had the last products' time to arrive
 #pragma unroll
-        for (int x = 0; x < TM; x++) sa[x] = na[x];
+        for (int x = 0; x < TM; x++) sa[x] = A::template ordered<WIDE>(na[x]);
 #pragma unroll
-        for (int x = 0; x < TN; x++) sb[x] = nb[x];
+        for (int x = 0; x < TN; x++) sb[x] = B::template ordered<WIDE>(nb[x]);
         slot = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -450,24 +461,25 @@ __global__ __launch_bounds__(256) void k_sum_shares(const float* __restrict__ pa
 
 // Which kernel takes a product, and how many shares of k: the least predicted time.  A workgroup of tiles takes ENDS_US to start and to write
 // its tile and STAGE_US a stage, the same alone on its compute unit as beside another one; shares cost a second launch and the traffic of
-// their sums.  Measured against the best of all plans at 39 shapes and formats of 64 to 4096 rows the choice is
-// within 8 %; 1003x700x2050, E4M3 by E2M1: tiles of 64 6.8 us, of 128 11.3, of 256 24; 2048x4096x4096 65, 44, 48; 4096x4096x4096 118, 85, 61.
+// their sums.  Against the best of all plans, at 64 shapes and formats of 40 to 8192
+// rows, it is within 5 % in 60 of them and 16 % off at worst; 1003x700x2050, E4M3 by E2M1: tiles of 64 6.5 us, of 128 11.0, of 256 24; 2048x4096x4096
+// 65, 43.5, 45; 4096x4096x4096 118, 87, 59.5.
 enum { ROWS_16, ROWS_32, TILES_64, TILES_128, TILES_256 };
 struct MxPlan { int kernel, split; };
 constexpr int CUS = 256;
+static long tiles_of(const MxProduct& p, int b) { return (long)((p.M + b - 1) / b) * ((p.N + b - 1) / b); }
 static MxPlan plan(const MxProduct& p) {
     if (p.M <= 16) return {ROWS_16, 1};
     if (p.M <= 32) return {ROWS_32, 1};
     const bool four = p.fa == MX_E2M1 && p.fb == MX_E2M1;
-    constexpr float STAGE_US[3][3] = {{0.33f, 0.82f, 2.2f}, {0.26f, 0.65f, 1.85f}, {0.58f, 1.1f, 3.4f}};   // E2M1 (256 k), E4M3 (128 k), widened (128 k)
+    constexpr float STAGE_US[3][3] = {{0.32f, 0.78f, 2.15f}, {0.26f, 0.65f, 1.85f}, {0.53f, 1.1f, 3.4f}};   // E2M1 (256 k), E4M3 (128 k), widened (128 k)
     constexpr float ENDS_US[3] = {0.7f, 2.2f, 3.5f};
     const float* const us = STAGE_US[four ? 0 : p.f32 ? 2 : 1];
     const int stages = (p.K + (four ? 255 : 127)) / (four ? 256 : 128);
     MxPlan best{TILES_64, 1};
     float least = 0.f;
     for (int i = 0; i < 3; i++) {
-        const int b = 64 << i;
-        const long tiles = (long)((p.M + b - 1) / b) * ((p.N + b - 1) / b);
+        const long tiles = tiles_of(p, 64 << i);
         for (int split = 1; split <= 16 && (split == 1 || (stages >= 2 * split && tiles * split <= 2 * CUS)); split *= 2) {
             const long rounds = (tiles * split + CUS - 1) / CUS;
             float t = 2.f + (float)rounds * (ENDS_US[i] + (float)((stages + split - 1) / split) * us[i]);
@@ -519,6 +531,12 @@ static hipError_t launch_rows(const MxProduct& q, hipStream_t st) {
     return hipGetLastError();
 }
 
+// The kernel and the shares of k of a product, 100 kernel + shares: for tests, not in the public headers.
+extern "C" int hh_internal_mx_plan(int m, int n, int k, int a_format, int b_format, int f32) {
+    const MxPlan l = plan(MxProduct{m, n, k, a_format, b_format, {}, {}, nullptr, n, f32, 0});
+    return 100 * l.kernel + l.split;
+}
+
 size_t mx_product_workspace(const MxProduct& p) {
     const MxPlan l = plan(p);
     return l.split > 1 ? (size_t)l.split * p.M * p.N * sizeof(float) : 0;
@@ -526,13 +544,19 @@ size_t mx_product_workspace(const MxProduct& p) {
 
 template <int FA, int FB, bool WIDE, typename TC>
 static hipError_t run_product(const MxProduct& p, void* ws, hipStream_t st) {
+    // Stages: three hide a request's way where LDS has room for them, which it has where one side is half the bytes (4096x8192x12288 E4M3 by
+    // E2M1 322 -> 306 us), for tiles of 64 (four are 2 % slower, two up to 30 %), and for one workgroup of tiles of 128 on a compute unit
+    // (2048x2048x8192 E4M3 57.4 -> 45.0), where a second one does so too (2048x4096x4096, two of them: 47.7, one at a time 50.3).
+    constexpr int NS = FA == FB ? 2 : 3;
     const MxPlan l = plan(p);
     switch (l.kernel) {
         case ROWS_16: return launch_rows<FA, FB, WIDE, TC, 1>(p, st);
         case ROWS_32: return launch_rows<FA, FB, WIDE, TC, 2>(p, st);
-        case TILES_64: return launch_tiles<FA, FB, WIDE, TC, 64, 64, 2, 2, 4>(p, l.split, ws, st);
-        case TILES_128: return launch_tiles<FA, FB, WIDE, TC, 128, 128, 2, 2, 2>(p, l.split, ws, st);
-        default: return launch_tiles<FA, FB, WIDE, TC, 256, 256, 2, 4, 2>(p, l.split, ws, st);
+        case TILES_64: return launch_tiles<FA, FB, WIDE, TC, 64, 64, 2, 2, 3>(p, l.split, ws, st);
+        case TILES_128:
+            if (NS == 3 || tiles_of(p, 128) * l.split <= CUS) return launch_tiles<FA, FB, WIDE, TC, 128, 128, 2, 2, 3>(p, l.split, ws, st);
+            return launch_tiles<FA, FB, WIDE, TC, 128, 128, 2, 2, 2>(p, l.split, ws, st);
+        default: return launch_tiles<FA, FB, WIDE, TC, 256, 256, 2, 4, NS>(p, l.split, ws, st);
     }
 }
 hipError_t mx_product(const MxProduct& p, void* ws, hipStream_t st) {

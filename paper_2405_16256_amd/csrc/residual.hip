@@ -6,7 +6,7 @@
 namespace hh {
 
 // ------------------------------------------------------------------ dropout
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void k_dropout(Drop d, int chunks, Divisor per_row, int cols, const T* x, long ldx, T* y, long ldy) {
     const int i = (int)(blockIdx.x * 256u + threadIdx.x);
     if (i >= chunks) return;
@@ -14,22 +14,24 @@ __global__ __launch_bounds__(256) void k_dropout(Drop d, int chunks, Divisor per
     const int group = split_off(row, per_row), n = cols - 8 * group;
     const long at = 8L * group;
     Eight<T> e;
-    e.load(x + row * ldx + at, n);
+    e.template load<STREAM>(x + row * ldx + at, n);
     float v[8];
     e.widen(v);
     drop8(d, drop_offset(d), (uint32_t)group, (uint32_t)row, v);
     e.round(v);
-    e.store(y + row * ldy + at, n);
+    e.template store<STREAM>(y + row * ldy + at, n);
 }
 
 hipError_t dropout(int dtype, const Drop& d, long rows, long cols, const void* x, long ldx, void* y, long ldy, hipStream_t st) {
     const int per_row = (int)((cols + 7) / 8), chunks = (int)(rows * per_row);
     const unsigned grid = ((unsigned)chunks + 255u) / 256u;
-    if (dtype == DT_BF16)
-        k_dropout<bf16_t><<<grid, 256, 0, st>>>(d, chunks, divisor(per_row), (int)cols, (const bf16_t*)x, ldx, (bf16_t*)y, ldy);
-    else
-        k_dropout<float><<<grid, 256, 0, st>>>(d, chunks, divisor(per_row), (int)cols, (const float*)x, ldx, (float*)y, ldy);
-    return hipGetLastError();
+    const bool stream = 2.0 * rows * cols * dt_size(dtype) > STREAM_BYTES;
+    auto run = [&](auto kern, auto* from, auto* to) {
+        kern<<<grid, 256, 0, st>>>(d, chunks, divisor(per_row), (int)cols, from, ldx, to, ldy);
+        return hipGetLastError();
+    };
+    if (dtype == DT_BF16) return run(stream ? k_dropout<bf16_t, true> : k_dropout<bf16_t, false>, (const bf16_t*)x, (bf16_t*)y);
+    return run(stream ? k_dropout<float, true> : k_dropout<float, false>, (const float*)x, (float*)y);
 }
 
 // ------------------------------------------------------------------ residual and norm
@@ -43,7 +45,7 @@ template <bool RAGGED> __device__ __forceinline__ int chunk_values(int hidden, i
 template <typename T> __device__ __forceinline__ T* chunk_at(T* row, int at) { return (T*)((char*)row + (uint32_t)at * (uint32_t)sizeof(T)); }
 template <typename T> __device__ __forceinline__ const T* chunk_at(const T* row, int at) { return (const T*)((const char*)row + (uint32_t)at * (uint32_t)sizeof(T)); }
 
-template <typename T, int W, int CH, bool RAGGED>
+template <typename T, int W, int CH, bool RAGGED, bool STREAM>
 __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int rows, int hidden, int width, float eps, const T* x, const T* b,
                                                                      const T* __restrict__ g, T* h, T* xn, int format, uint8_t* codes, uint8_t* scales) {
     __shared__ float red[W];
@@ -63,8 +65,8 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
         rb[c] = Eight<T>{};
         rg[c] = Eight<T>{};
         if (n > 0) {
-            rx[c].load(chunk_at(x_row, at), n);
-            if (b) rb[c].load(chunk_at(b_row, at), n);
+            rx[c].template load<STREAM>(chunk_at(x_row, at), n);
+            if (b) rb[c].template load<STREAM>(chunk_at(b_row, at), n);
             rg[c].load(chunk_at(g, at), n);
         }
     }
@@ -81,7 +83,7 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
 #pragma unroll
             for (int i = 0; i < 8; i++) v[c][i] += u[i];
             rx[c].round(v[c]);
-            rx[c].store(chunk_at(h_row, 8 * group), n);
+            rx[c].template store<STREAM>(chunk_at(h_row, 8 * group), n);
             rx[c].widen(v[c]);   // the norm is of the sum as it is kept
         }
 #pragma unroll
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
         if (xn && n > 0) {
             Eight<T> e;
             e.round(u);
-            e.store(chunk_at(xn_row, 8 * group), n);
+            e.template store<STREAM>(chunk_at(xn_row, 8 * group), n);
         }
         if (format != MX_NONE && 8 * group < width) {   // whole blocks of 32: the four lanes of one are here together
             const uint32_t m = quad_max(magnitude8(u));
@@ -122,13 +124,16 @@ template <typename T>
 static hipError_t fwd(const Drop& d, int rows, int hidden, float eps, const void* x, const void* b, const void* g, void* h, void* xn, int format,
                       const MxRows& q, hipStream_t st) {
     const int width = format == MX_NONE ? 0 : (int)mx_width(hidden), chunks = format == MX_NONE ? (hidden + 7) / 8 : width / 8;
+    const bool stream = (double)rows * hidden * sizeof(T) * (1 + 2 * (b != nullptr) + (xn != nullptr)) > STREAM_BYTES;
     auto run = [&](auto kern, int each, int threads) {
         kern<<<(rows + each - 1) / each, threads, 0, st>>>(d, rows, hidden, width, eps, (const T*)x, (const T*)b, (const T*)g, (T*)h, (T*)xn, format,
                                                            q.codes, q.scales);
         return hipGetLastError();
     };
 #define HH_SHAPE(W, CH) \
-    if (chunks <= 64 * W * CH) return hidden % 8 ? run(k_add_norm_fwd<T, W, CH, true>, rows_each<W>(), row_threads<W>()) : run(k_add_norm_fwd<T, W, CH, false>, rows_each<W>(), row_threads<W>())
+    if (chunks <= 64 * W * CH)                            \
+        return run(hidden % 8 ? k_add_norm_fwd<T, W, CH, true, false> : stream ? k_add_norm_fwd<T, W, CH, false, true> : k_add_norm_fwd<T, W, CH, false, false>, \
+                   rows_each<W>(), row_threads<W>())
     // Few rows take more waves each: the chip is not full, and a row's own chain is what they wait for (700x1003 fp32 5.6 -> 4.8 us, 2000x1024
     // bf16 the other way 4.8 -> 5.1; 200x8192 bf16 5.1 -> 4.7, 2048x4096 12.0 with 4 waves).
     HH_SHAPE(1, 1);
@@ -173,7 +178,7 @@ __device__ __forceinline__ void row_sums(float& ss, float& dot, float (&red)[2][
 // Registers of bf16 rows are held to what leaves four waves on a SIMD: a row's loads wait for no one but themselves, and the other waves'
 // cover them.
 template <typename T, int CH> constexpr int grad_waves() { return sizeof(T) == 2 && CH <= 3 ? 4 : 2; }
-template <typename T, int W, int CH, bool RAGGED>
+template <typename T, int W, int CH, bool RAGGED, bool STREAM>
 __global__ __launch_bounds__(row_threads<W>(), (RAGGED ? 2 : grad_waves<T, CH>())) void k_add_norm_bwd(Drop d, int rows, int hidden, int parts, float eps, const T* h,
                                                                                           const T* __restrict__ g, const T* dxn, const T* dh, T* dx, T* db,
                                                                                           float* __restrict__ partial) {
@@ -207,9 +212,9 @@ __global__ __launch_bounds__(row_threads<W>(), (RAGGED ? 2 : grad_waves<T, CH>()
             ru[c] = Eight<T>{};
             rd[c] = Eight<T>{};
             if (n > 0) {
-                rh[c].load(chunk_at(h_row, at), n);
-                ru[c].load(chunk_at(dxn_row, at), n);
-                if (dh) rd[c].load(chunk_at(dh_row, at), n);
+                rh[c].template load<STREAM>(chunk_at(h_row, at), n);
+                ru[c].template load<STREAM>(chunk_at(dxn_row, at), n);
+                if (dh) rd[c].template load<STREAM>(chunk_at(dh_row, at), n);
             }
         }
         float ss = 0.f, dot = 0.f;
@@ -242,11 +247,11 @@ __global__ __launch_bounds__(row_threads<W>(), (RAGGED ? 2 : grad_waves<T, CH>()
             norm_grad8(a, u, w, o, sum[c], r, k);
             Eight<T> e;
             e.round(o);
-            e.store(chunk_at(dx_row, 8 * group), n);
+            e.template store<STREAM>(chunk_at(dx_row, 8 * group), n);
             if (db) {
                 if (d.dropped) drop8(d, offset, (uint32_t)group, (uint32_t)row, o);
                 e.round(o);
-                e.store(chunk_at(db_row, 8 * group), n);
+                e.template store<STREAM>(chunk_at(db_row, 8 * group), n);
             }
         }
     }
@@ -373,12 +378,15 @@ template <typename T>
 static hipError_t bwd(const Drop& d, int rows, int hidden, float eps, const void* h, const void* g, const void* dxn, const void* dh, void* dx, void* db,
                       float* partial, hipStream_t st) {
     const int chunks = (hidden + 7) / 8, parts = add_norm_partial_rows(rows, hidden);
+    const bool stream = (double)rows * hidden * sizeof(T) * (3 + (dh != nullptr) + (db != nullptr)) > STREAM_BYTES;
     auto run = [&](auto kern, int threads) {
         kern<<<parts, threads, 0, st>>>(d, rows, hidden, parts, eps, (const T*)h, (const T*)g, (const T*)dxn, (const T*)dh, (T*)dx, (T*)db, partial);
         return hipGetLastError();
     };
 #define HH_SHAPE(W, CH) \
-    if (chunks <= 64 * W * CH) return hidden % 8 ? run(k_add_norm_bwd<T, W, CH, true>, row_threads<W>()) : run(k_add_norm_bwd<T, W, CH, false>, row_threads<W>())
+    if (chunks <= 64 * W * CH)                            \
+        return run(hidden % 8 ? k_add_norm_bwd<T, W, CH, true, false> : stream ? k_add_norm_bwd<T, W, CH, false, true> : k_add_norm_bwd<T, W, CH, false, false>, \
+                   row_threads<W>())
     HH_SHAPE(1, 1); HH_SHAPE(1, 2);
     HH_SHAPE(4, 1); HH_SHAPE(8, 1); HH_SHAPE(8, 2); HH_SHAPE(8, 3);
     if constexpr (sizeof(T) == 2) HH_SHAPE(8, 4);

@@ -79,6 +79,27 @@ class Packed:
         return q
 
 
+def drawn(rng, rows, k, fmt):
+    """A packed tensor of blocks drawn from those of a smaller one, and its values: for sizes at which packing on the host takes seconds."""
+    f = FORMATS[fmt][0]
+    codes, scales = O.quantise(rng.standard_normal((64, 4096)), f)
+    width = -(-k // 256) * 256
+    pick = rng.integers(0, scales.size, (rows, width // 32))
+    c, s = codes.reshape(-1, 32)[pick].reshape(rows, width), scales.reshape(-1)[pick]
+    c[:, k:] = 0
+    s[:, -(-k // 32):] = 0
+    q = Packed(rows, k, fmt)
+    q.codes[:q.c] = torch.from_numpy(O.in_memory(c, f).reshape(-1)).to(L.DEV)
+    q.scales[:q.s] = torch.from_numpy(s.reshape(-1)).to(L.DEV)
+    return q, O.values(c, s, k, f)
+
+
+def sums(a, b):
+    """a b^T in fp64."""
+    a, b = (torch.from_numpy(np.ascontiguousarray(t)).to(L.DEV) for t in (a, b.T))
+    return (a @ b).cpu().numpy()
+
+
 def within(got, want, bound, what):
     d = np.abs(got - want)
     worst = np.unravel_index(np.argmax(d - bound), d.shape)
@@ -359,6 +380,48 @@ def test_rows_behind_the_last_are_left_alone(ctx):
         assert torch.equal(t[5:], u[5:])
 
 
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("hidden", (1000, 4096, 12288))
+def test_tensors_past_the_caches(ctx, dtype, hidden):
+    """Rows of a tensor that is streamed past the caches have the bits that they have in a smaller one, of 1024 rows: with fewer a row is summed by
+    more lanes, in another order."""
+    dt, code = TYPES[dtype]
+    rows = int(1.4e8 / hidden / (2 if dtype == "bf16" else 4)) // 2 * 2 + 1
+    gen = torch.Generator(device=L.DEV)
+    gen.manual_seed(hidden)
+    x, b, d, o = (torch.randn(rows, hidden, dtype=dt, device=L.DEV, generator=gen) for _ in range(4))
+    g = torch.randn(hidden, dtype=dt, device=L.DEV, generator=gen)
+
+    def all_of(n, x, b, d, o, drop):
+        q, c = Packed(n, hidden, "e4m3"), Packed(hidden, n, "e2m1")
+        r = {k: torch.empty_like(x) for k in ("h", "xn", "dx", "db", "y", "v")}
+        cfg = hh.make_add_norm_cfg(n, hidden, 1e-5, code, hh.HH_MX_E4M3)
+        dg, ws = torch.empty(hidden, device=L.DEV), torch.empty(hh.hh_add_norm_sizes(cfg), dtype=torch.uint8, device=L.DEV)
+        st = L.stream_ptr()
+        hh.hh_add_norm_fwd(ctx, cfg, drop, x, b, g, r["h"], r["xn"], q.struct, st)
+        hh.hh_add_norm_bwd(ctx, cfg, drop, r["h"], g, d, o, r["dx"], r["db"], dg, 0, ws, st)
+        hh.hh_dropout(ctx, hh.make_dropout(0.25, 2), n, hidden, code, x, hidden, r["y"], hidden, st)
+        hh.hh_mx_quantise(ctx, n, hidden, code, x, hidden, hh.HH_MX_E2M1, None, c.struct, st)
+        hh.hh_mx_values(ctx, n, hidden, hh.HH_MX_E4M3, q.struct, code, r["v"], hidden, st)
+        p = Packed(n, hidden, "e4m3")
+        hh.hh_mx_quantise(ctx, n, hidden, code, x, hidden, hh.HH_MX_E4M3, p.struct, None, st)
+        torch.cuda.synchronize()
+        r["codes"], r["scales"] = q.codes[:q.c].view(n, -1), q.scales[:q.s].view(n, -1)
+        r["p"], r["ps"] = p.codes[:p.c].view(n, -1), p.scales[:p.s].view(n, -1)
+        return r, c.codes[:c.c].view(hidden, -1), dg
+    big, columns, dg = all_of(rows, x, b, d, o, hh.make_dropout(0.25, 1))
+    top, few, _ = all_of(1024, x[:1024], b[:1024], d[:1024], o[:1024], hh.make_dropout(0.25, 1))
+    for k, t in top.items():
+        assert torch.equal(big[k][:1024], t), k
+    assert torch.equal(columns[:, :512], few)
+    last, _, _ = all_of(1, x[-1:], b[-1:], d[-1:], o[-1:], None)
+    for k in ("p", "ps"):
+        assert torch.equal(big[k][-1:], last[k]), k
+    h, u = big["h"].double(), d.double()
+    term = u * h / torch.sqrt(torch.mean(h * h, dim=1, keepdim=True) + float(np.float32(1e-5)))
+    assert bool(((dg - term.sum(0)).abs() <= (rows + 48) * E * term.abs().sum(0)).all())
+
+
 # ------------------------------------------------------------------ product
 def check_product(ctx, m, n, k, fa, fb, dtype, extra=0, accumulate=False, spread=0, seed=0):
     rng = np.random.default_rng(seed + m + 3 * n + 5 * k)
@@ -368,9 +431,12 @@ def check_product(ctx, m, n, k, fa, fb, dtype, extra=0, accumulate=False, spread
         if spread:
             t = t * np.exp2(rng.integers(-spread, spread, (rows, k)))
         return t
-    a, b = operand(m), operand(n)
-    qa, qb = Packed.of(a, fa), Packed.of(b, fb)
-    va, vb = O.rounded(a, FORMATS[fa][0]), O.rounded(b, FORMATS[fb][0])
+    if (m + n) * k > 1 << 20:
+        (qa, va), (qb, vb) = drawn(rng, m, k, fa), drawn(rng, n, k, fb)
+    else:
+        a, b = operand(m), operand(n)
+        qa, qb = Packed.of(a, fa), Packed.of(b, fb)
+        va, vb = O.rounded(a, FORMATS[fa][0]), O.rounded(b, FORMATS[fb][0])
     c = torch.full((m + 2, n + extra), 7.0, dtype=TYPES[dtype][0], device=L.DEV)
     old = rng.standard_normal((m, n)).astype(np.float32) if accumulate else np.zeros((m, n))
     if accumulate:
@@ -383,8 +449,8 @@ def check_product(ctx, m, n, k, fa, fb, dtype, extra=0, accumulate=False, spread
     got = np64(c)
     assert (got[m:] == 7.0).all() and (got[:, n:] == 7.0).all() and (ws[-256:] == JUNK).all()
     got = got[:m, :n]
-    want = va @ vb.T + old
-    size = np.abs(va) @ np.abs(vb).T
+    want = sums(va, vb) + old
+    size = sums(np.abs(va), np.abs(vb))
     coarse = "e4m3" in (fa, fb) and dtype == "bf16"
     within(got, want, (2.0 ** -10 if coarse else 2 * k * E) * size + 2 * E * np.abs(old) + HALF[dtype] * np.abs(want), "product")
     # roundings of either sign grow with the root of their number, each of a sum that grows with the root of its terms
@@ -412,7 +478,7 @@ def test_product_adds_to_what_is_there(ctx, dtype, fa, fb):
 
 
 @pytest.mark.parametrize("fa,fb", PAIRS)
-@pytest.mark.parametrize("m,n,k", [(256, 512, 2048), (1024, 768, 1280), (2047, 1030, 900), (700, 5000, 4100), (3000, 2900, 700)])
+@pytest.mark.parametrize("m,n,k", [(256, 512, 2048), (1024, 768, 1280), (2047, 1030, 900), (700, 5000, 4100), (3000, 2900, 700), (970, 1106, 5422), (1106, 4096, 7424)])
 def test_larger_products(ctx, m, n, k, fa, fb):
     for dtype in ("bf16", "f32"):
         check_product(ctx, m, n, k, fa, fb, dtype)

@@ -155,6 +155,22 @@ def test_product_refuses():
     assert hh.lib.hh_mx_product_sizes(None, None) == BAD
 
 
+# ------------------------------------------------------------------ plans of the product
+def test_every_kernel_of_the_product_is_tested():
+    """The sizes of the GPU tests reach each kernel, whole and in shares of k, with one workgroup on a compute unit and with several."""
+    def plan(m, n, k, fa, fb, f32):
+        v = hh.lib.hh_internal_mx_plan(m, n, k, fa, fb, int(f32))
+        return v // 100, v % 100
+    from tests import test_gpu_mx as G
+    sizes = [s for t in (G.test_product, G.test_larger_products) for mark in t.pytestmark if mark.name == "parametrize" and mark.args[0] == "m,n,k" for s in mark.args[1]]
+    seen = {plan(m, n, k, fa, fb, f32) for m, n, k in sizes for fa in (1, 2) for fb in (1, 2) for f32 in (0, 1)}
+    assert {k for k, _ in seen} == set(range(5)) and {k for k, s in seen if s > 1} == {2, 3, 4}, seen
+    many = {plan(m, n, k, 1, 1, 0)[0] for m, n, k in sizes if -(-m // 128) * -(-n // 128) > 256}
+    assert 3 in {plan(*s, 1, 1, 0)[0] for s in sizes} and many, many
+    for m in (1, 16, 17, 32, 33):      # rows of their own up to 32
+        assert plan(m, 4096, 4096, 1, 2, 0)[0] == (0 if m <= 16 else 1 if m <= 32 else 2)
+
+
 # ------------------------------------------------------------------ pins of the definitions
 def test_generator_gives_its_authors_known_answers():
     """Counter, key and result as published with the generator."""
