@@ -254,7 +254,8 @@ typedef enum {
     HH_TRACE_ATTN_FWD = 3,
     HH_TRACE_ATTN_BWD = 4,
     HH_TRACE_ELEMENTWISE = 5,  /* RMSNorm, RoPE, SwiGLU (unless a small layer's GEMM does the latter two), gain-gradient reduction,
-                                  everything of hh_train.h but its GEMMs */
+                                  everything of hh_train.h but its GEMMs, of hh_mx.h but its product
+                                  (HH_TRACE_GEMM_NT) */
     HH_TRACE_KINDS = 6
 } hh_trace_kind;
 typedef struct {
