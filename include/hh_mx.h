@@ -11,7 +11,8 @@
  *
  * The general rules of hh.h hold: statuses and hh_last_error(), device pointers of 16-byte alignment, buffers that the caller owns, work
  * enqueued on `stream` without synchronisation, allocation or copies, checks of arguments before any of it.  The context's device has to
- * be the calling thread's current one (HH_ERR_INVALID_ARG otherwise).  Every result is the same from run to run, bit for bit.
+ * be the calling thread's current one (HH_ERR_INVALID_ARG otherwise).  Every result is the same from run to run, bit for bit;
+ * a row's sums may be added in another order in a call with another number of rows.  Two calls that may run at the same time need a workspace each.
  */
 #ifndef HH_MX_H
 #define HH_MX_H
@@ -66,7 +67,8 @@ int hh_mx_sizes(int32_t format, int64_t rows, int64_t k, size_t *codes_bytes, si
 int hh_mx_quantise(hh_ctx *ctx, int64_t rows, int64_t cols, int32_t dtype, const void *x, int64_t ldx, int32_t format,
                    const hh_mx_tensor *by_row, const hh_mx_tensor *by_column, void *stream);
 
-/* The values [rows, k] that a packed tensor stands for, in dtype, rows ldy elements apart.  bfloat16 holds them exactly. */
+/* The values [rows, k] that a packed tensor stands for, in dtype, rows ldy elements apart.  bfloat16 holds them exactly, but for E4M3
+ * values below 2^-133. */
 int hh_mx_values(hh_ctx *ctx, int64_t rows, int64_t k, int32_t format, const hh_mx_tensor *q, int32_t dtype, void *y, int64_t ldy,
                  void *stream);
 
@@ -88,7 +90,7 @@ int hh_add_norm_fwd(hh_ctx *ctx, const hh_add_norm_cfg *cfg, const hh_dropout_cf
  * on as if it were xn) and, where it is not NULL, the gradient dh that reaches h from elsewhere:
  *     u = dxn g,  r = 1 / sqrt(mean(h^2) + eps):   dx = dh + r (u - h r^2 mean(u h)),   db = dropout(dx),   dg (+)= sum over rows of dxn h r
  * db is of the dx that has not been rounded; NULL: it is not written (without dropout it is dx).  dg: [hidden] fp32, added to where
- * accumulate != 0; NULL: not wanted.  dx may be dh, dxn or h, db any of the others.  workspace of hh_add_norm_sizes bytes (only used for dg). */
+ * accumulate != 0; NULL: not wanted.  dx may be dh, dxn or h, and db any other one of them.  workspace of hh_add_norm_sizes bytes (only used for dg). */
 int hh_add_norm_sizes(const hh_add_norm_cfg *cfg, size_t *workspace_bytes);
 int hh_add_norm_bwd(hh_ctx *ctx, const hh_add_norm_cfg *cfg, const hh_dropout_cfg *drop, const void *h, const void *g, const void *dxn,
                     const void *dh, void *dx, void *db, float *dg, int accumulate, void *workspace, void *stream);
@@ -102,7 +104,7 @@ int hh_add_norm_bwd(hh_ctx *ctx, const hh_add_norm_cfg *cfg, const hh_dropout_cf
  * Into HH_F32 both operands are widened to bfloat16 instead, exactly, and multiplied at that type's rate: sums as exact as fp32 ones.
  * E2M1 on both sides: exact within an instruction, as exact as fp32 sums over k, into either type.
  *
- * A packed operand is below 2^32 - 2^25 bytes, c at most 2^33 elements.  workspace of hh_mx_product_sizes bytes, NULL where that is 0. */
+ * A packed operand is below 2^32 - 2^25 bytes, c at most 2^33 elements.  workspace of hh_mx_product_sizes bytes (128 MiB at most), NULL where that is 0. */
 typedef struct {
     int32_t m, n, k;
     int32_t a_format, b_format;

@@ -508,6 +508,32 @@ def test_blocks_that_are_no_numbers_reach_their_rows_alone(ctx, dtype, fa, fb, m
     assert np.array_equal(nan, want)
 
 
+@pytest.mark.parametrize("fa,fb", PAIRS)
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("m", (2, 300))
+def test_scales_at_their_ends(ctx, dtype, fa, fb, m):
+    """Codes of 1 under scales that a packer elsewhere may write: NaN, the least one against a large one, the largest against a small one."""
+    n, k = 290, 300
+    one = {"e4m3": 0x38, "e2m1": 0x02}
+
+    def operand(rows, fmt, scale):
+        q = Packed(rows, k, fmt)
+        codes = np.zeros((rows, 512), dtype=np.uint8)
+        codes[:, 5] = one[fmt]
+        scales = np.zeros((rows, 16), dtype=np.uint8)
+        scales[:, 0] = scale
+        q.codes[:q.c] = torch.from_numpy(O.in_memory(codes, FORMATS[fmt][0]).reshape(-1)).to(L.DEV)
+        q.scales[:q.s] = torch.from_numpy(scales.reshape(-1)).to(L.DEV)
+        return q
+    cfg = hh.make_mx_product_cfg(m, n, k, FORMATS[fa][1], FORMATS[fb][1], TYPES[dtype][1])
+    ws = torch.empty(hh.hh_mx_product_sizes(cfg), dtype=torch.uint8, device=L.DEV)
+    for sa, sb, want in ((255, 127, np.nan), (127, 255, np.nan), (0, 227, 2.0 ** -27), (227, 0, 2.0 ** -27), (1, 227, 2.0 ** -26), (240, 27, 2.0 ** 13), (27, 240, 2.0 ** 13)):
+        c = torch.zeros(m, n, dtype=TYPES[dtype][0], device=L.DEV)
+        qa, qb = operand(m, fa, sa), operand(n, fb, sb)
+        hh.hh_mx_product(ctx, cfg, qa.struct, qb.struct, c, 0, ws, L.stream_ptr())
+        assert np.array_equal(np64(c), np.full((m, n), want), equal_nan=True), (sa, sb, float(c[0, 0]))
+
+
 def test_operand_past_31_bits(ctx):
     m, n, k = 519000, 24, 8192                                  # 4.25e9 bytes
     a = Packed(m, k, "e4m3")
