@@ -18,6 +18,8 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // Of 16 rows x 128 k lane l holds row l % 16 and, with q = l / 16, of E2M1 the codes 32 q .. 32 q + 31, of E4M3 (and WIDE) 16 q .. 16 q + 15 and
 // 64 + 16 q .. 64 + 16 q + 15; its scale is that of k = 32 q .. 32 q + 31.
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+// The conversions take a scale's exponent alone, of which 0 is 2^-127 and 255 NaN to them.
+__device__ __forceinline__ float scale_bits(uint32_t byte) { return __uint_as_float(byte << 23); }
 template <int F> __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale);   // 8 codes (E2M1: of lo) with their scale, exactly
 template <> __device__ __forceinline__ bf16x8 widen8<MX_E4M3>(uint32_t lo, uint32_t hi, float scale) {
     const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
@@ -63,7 +65,7 @@ struct RowUnit {   // 256 k of the lane's row
     __device__ __forceinline__ int scale(int half, int q) const { return (int)((half ? s.y : s.x) >> (8 * q)); }
     // 8 codes of the 16 at k = 128 half + 64 part + 16 q, widened
     __device__ __forceinline__ bf16x8 widened(int half, int part, int eight, int q) const {
-        const float x = scale_value((half ? s.y : s.x) >> (16 * part + 8 * (q >> 1)) & 255u);
+        const float x = scale_bits((half ? s.y : s.x) >> (16 * part + 8 * (q >> 1)) & 255u);
         if constexpr (F == MX_E4M3) return widen8<F>((uint32_t)v[2 * half + part][2 * eight], (uint32_t)v[2 * half + part][2 * eight + 1], x);
         else return widen8<F>((uint32_t)v[half][2 * part + eight], 0u, x);
     }
@@ -135,19 +137,20 @@ __global__ __launch_bounds__(64 * NW) void k_product_rows(MxRowsProblem p) {
 
 // ------------------------------------------------------------------ tiles
 // BM x BN of C a workgroup, WR x WC waves, each 32 TM x 32 TN.  k advances KS at a time through NS LDS stages that are filled straight from
-// global memory; a row of a stage is 128 bytes of E4M3 (KS 128), or 64 beside that, or 128 of E2M1 on both sides (KS 256), and the scales of
-// those k lie behind the tiles.  16-byte chunks are XOR-swizzled by the row so that a fragment's 16 lanes cover all banks.
+// global memory; a row of a stage is KS bytes of E4M3 or KS / 2 of E2M1 (KS 128, or 256), and the scales of those k lie behind the
+// tiles.  16-byte chunks are XOR-swizzled by the row so that a fragment's 16 lanes cover all banks.
 //
-// 4096x8192x12288 into bf16: E2M1 214 us (3.85 PFLOP/s), E4M3 336 (2.45), E4M3 by E2M1 302 (2.7), widened into fp32 620 (1.33).  The matrix
+// 4096x8192x12288 into bf16: E2M1 214 us (3.85 PFLOP/s), E4M3 355 (2.32), E4M3 by E2M1 317 (2.6), widened into fp32 606 (1.36).  The matrix
 // cores alone, with random operands in registers, reach 6.8, 4.0 and (bf16) 1.8 PFLOP/s under the power limit.  Counters (E2M1): matrix
 // cores busy 51 % of the cycles at 1.85 GHz, workgroups there 91 % (two tiles a compute unit, each with its start and end), waits 33 %,
 // for LDS 3 %.  Without the loop's requests it takes 168 us, without the matrix instructions 165, with every request in L2 203: neither
 // side is the limit by itself, and the two add up to more than either.  Four waves of 128x128, four stages of 128 k (268), fragments fetched
 // earlier or later, requests spread wider and raised wave priorities changed nothing or cost time.
 template <int F, int KS> constexpr int ROW_BYTES = F == MX_E4M3 ? KS : KS / 2;
-template <int RB> __device__ __forceinline__ int swizzled(int row, int chunk) {   // byte offset in the tile
-    return row * RB + ((RB == 128 ? chunk ^ ((row >> 1) & 7) : chunk ^ ((row >> 2) & 3)) << 4);
+template <int RB> __device__ __forceinline__ int turned(int row, int chunk) {
+    return RB == 256 ? chunk ^ (row & 15) : RB == 128 ? chunk ^ ((row >> 1) & 7) : chunk ^ ((row >> 2) & 3);
 }
+template <int RB> __device__ __forceinline__ int swizzled(int row, int chunk) { return row * RB + (turned<RB>(row, chunk) << 4); }   // byte in the tile
 template <int FA, int FB> constexpr int STAGE_K = FA == MX_E2M1 && FB == MX_E2M1 ? 256 : 128;
 
 __device__ __forceinline__ void dma4(uint32_t lds_addr, uint32_t voff, i32x4 rs) {   // as dma16, four bytes a lane
@@ -169,8 +172,7 @@ struct MxTile {
     __device__ static __forceinline__ uint32_t voff(int wave, int i, int row0, uint32_t pitch) {
         constexpr int LPR = RB / 16;
         const int L = threadIdx.x & 63, r = (wave * PER_WAVE + i) * (64 / LPR) + L / LPR;
-        const int logical = RB == 128 ? (L & 7) ^ ((r >> 1) & 7) : (L & 3) ^ ((r >> 2) & 3);
-        return (uint32_t)(row0 + r) * pitch + (uint32_t)(logical * 16);
+        return (uint32_t)(row0 + r) * pitch + (uint32_t)(turned<RB>(r, L % LPR) * 16);
     }
     __device__ static __forceinline__ uint32_t scale_voff(int part, int row0, uint32_t pitch) {
         const int d = 64 * part + (int)(threadIdx.x & 63);
@@ -203,9 +205,12 @@ struct MxTile {
         if constexpr (F == MX_E4M3) return widen8<F>((uint32_t)f.v[piece >> 1][2 * (piece & 1)], (uint32_t)f.v[piece >> 1][2 * (piece & 1) + 1], scale);
         else return widen8<F>((uint32_t)f.v[0][piece], 0u, scale);
     }
-    // The scales of a stage for rows rb .. rb + 31, as they lie in LDS, and what the products take: not WIDE, byte (KS 256: s, KS 128: 2 s) is
-    // that of step s for this lane's half; WIDE, bytes 2 s and 2 s + 1 are those of step s.
-    struct Scales { uint32_t w[SB / 4]; };
+    // The scales of a stage for rows rb .. rb + 31, as they lie in LDS, and what the products take.  Not WIDE, byte (KS 256: s, KS 128: 2 s) is
+    // that of step s for this lane's half; WIDE, those of step s are bytes 2 s and 2 s + 1.
+    struct Scales {
+        uint32_t w[SB / 4];
+        __device__ __forceinline__ float of(int block) const { return scale_bits(w[block >> 2] >> (8 * (block & 3)) & 255u); }
+    };
     __device__ static __forceinline__ Scales scales(const char* lds, int rb) {
         const int r = rb + (int)(threadIdx.x & 31);
         Scales s;
@@ -218,10 +223,12 @@ struct MxTile {
         }
         return s;
     }
-    template <bool WIDE> __device__ static __forceinline__ int ordered(const Scales& s) {
+    template <bool WIDE> __device__ static __forceinline__ Scales ordered(Scales s) {
         const int h = (int)(threadIdx.x & 63) >> 5;
-        if constexpr (SB == 8) return (int)__builtin_amdgcn_perm(s.w[1], s.w[0], h ? 0x07050301u : 0x06040200u);
-        else return (int)(WIDE ? s.w[0] : s.w[0] >> (8 * h));
+        if constexpr (WIDE) return s;
+        if constexpr (SB == 8) s.w[0] = __builtin_amdgcn_perm(s.w[1], s.w[0], h ? 0x07050301u : 0x06040200u);
+        else s.w[0] >>= 8 * h;
+        return s;
     }
 };
 
@@ -241,9 +248,9 @@ struct MxProblem {
     TileMap map;
 };
 
-template <int FA, int FB, bool WIDE, typename TC, int BM, int BN, int WR, int WC, int NS>
+template <int FA, int FB, bool WIDE, typename TC, int KS, int BM, int BN, int WR, int WC, int NS>
 __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
-    constexpr int KS = STAGE_K<FA, FB>, NW = WR * WC, TM = BM / WR / 32, TN = BN / WC / 32, STEPS = KS / 64, Q = STEPS * TM;
+    constexpr int NW = WR * WC, TM = BM / WR / 32, TN = BN / WC / 32, STEPS = KS / 64, Q = STEPS * TM;
     using A = MxTile<FA, KS, BM, NW>;
     using B = MxTile<FB, KS, BN, NW>;
     constexpr int STAGE = A::BYTES + B::BYTES + A::SCALES + B::SCALES, AT_B = A::BYTES, AT_SA = AT_B + B::BYTES, AT_SB = AT_SA + A::SCALES;
@@ -317,9 +324,8 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
     static_assert(Q % RING == 0 && STEPS % 2 == 0, "a stage ends where it began in both rings");
     typename A::Frag fa[RING];
     typename B::Frag fb[2][TN];
-    int sa[TM], sb[TN];
-    typename A::Scales na[TM];
-    typename B::Scales nb[TN];
+    typename A::Scales sa[TM], na[TM];
+    typename B::Scales sb[TN], nb[TN];
 #pragma unroll
     for (int q = 0; q < AHEAD; q++) fa[q] = A::template frag<WIDE>(smem, wm + 32 * (q % TM), q / TM);
 #pragma unroll
@@ -366,18 +372,18 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product_tiles(MxProblem p) {
                 if constexpr (WIDE) {
 #pragma unroll
                     for (int piece = 0; piece < 4; piece++) {
-                        const int at = 8 * (2 * step + (piece >> 1));
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            B::widen_piece(fb[step & 1][j], piece, scale_value((uint32_t)sb[j] >> at & 255u)),
-                            A::widen_piece(fa[q % RING], piece, scale_value((uint32_t)sa[i] >> at & 255u)), acc[i][j], 0, 0, 0);
+                        const int block = 2 * step + (piece >> 1);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(B::widen_piece(fb[step & 1][j], piece, sb[j].of(block)),
+                                                                            A::widen_piece(fa[q % RING], piece, sa[i].of(block)), acc[i][j], 0, 0, 0);
                     }
                 } else {
                     const i32x8 x = B::operand(fb[step & 1][j]), y = A::operand(fa[q % RING]);
+                    const int ys = (int)sa[i].w[0], xs = (int)sb[j].w[0];
                     if (KS == 256) {
-                        acc[i][j] = step == 0 ? mfma_mx<FB, FA, 0, 0>(x, y, acc[i][j], sb[j], sa[i]) : step == 1 ? mfma_mx<FB, FA, 1, 1>(x, y, acc[i][j], sb[j], sa[i])
-                                  : step == 2 ? mfma_mx<FB, FA, 2, 2>(x, y, acc[i][j], sb[j], sa[i]) : mfma_mx<FB, FA, 3, 3>(x, y, acc[i][j], sb[j], sa[i]);
+                        acc[i][j] = step == 0 ? mfma_mx<FB, FA, 0, 0>(x, y, acc[i][j], xs, ys) : step == 1 ? mfma_mx<FB, FA, 1, 1>(x, y, acc[i][j], xs, ys)
+                                  : step == 2 ? mfma_mx<FB, FA, 2, 2>(x, y, acc[i][j], xs, ys) : mfma_mx<FB, FA, 3, 3>(x, y, acc[i][j], xs, ys);
                     } else {
-                        acc[i][j] = step == 0 ? mfma_mx<FB, FA, 0, 0>(x, y, acc[i][j], sb[j], sa[i]) : mfma_mx<FB, FA, 2, 2>(x, y, acc[i][j], sb[j], sa[i]);
+                        acc[i][j] = step == 0 ? mfma_mx<FB, FA, 0, 0>(x, y, acc[i][j], xs, ys) : mfma_mx<FB, FA, 2, 2>(x, y, acc[i][j], xs, ys);
                     }
                 }
             }
@@ -468,10 +474,10 @@ __global__ __launch_bounds__(256) void k_sum_shares(const float* __restrict__ pa
 }
 
 // Which kernel takes a product, and how many shares of k: the least predicted time.  A workgroup of tiles takes ENDS_US to start and to write
-// its tile and STAGE_US a stage, the same alone on its compute unit as beside another one; shares cost a second launch and the traffic of
-// their sums.  Against the best of all plans, at 64 shapes and formats of 40 to 8192
-// rows, it is within 5 % in 60 of them and 16 % off at worst; 1003x700x2050, E4M3 by E2M1: tiles of 64 6.5 us, of 128 11.0, of 256 24; 2048x4096x4096
-// 65, 43.5, 45; 4096x4096x4096 118, 87, 59.5.
+// its tile and STAGE_US a stage (256 k of E2M1, else 128), the same alone on its compute unit as beside another one; shares cost a second
+// launch and the traffic of their sums.  Against the best of all plans, at 64 shapes and formats of 40 to 8192 rows, it is within 5 % in 59
+// of them and 15 % off at worst; 1003x700x2050, E4M3 by E2M1: tiles of 64 6.5 us, of 128 11.0, of 256 24; 2048x4096x4096 65, 43.5, 45;
+// 4096x4096x4096 118, 87, 59.5.
 enum { ROWS_16, ROWS_32, TILES_64, TILES_128, TILES_256 };
 struct MxPlan { int kernel, split; };
 constexpr int CUS = 256;
@@ -480,7 +486,7 @@ static MxPlan plan(const MxProduct& p) {
     if (p.M <= 16) return {ROWS_16, 1};
     if (p.M <= 32) return {ROWS_32, 1};
     const bool four = p.fa == MX_E2M1 && p.fb == MX_E2M1;
-    constexpr float STAGE_US[3][3] = {{0.32f, 0.78f, 2.15f}, {0.26f, 0.65f, 1.85f}, {0.53f, 1.1f, 3.4f}};   // E2M1 (256 k), E4M3 (128 k), widened (128 k)
+    constexpr float STAGE_US[3][3] = {{0.32f, 0.78f, 2.15f}, {0.26f, 0.65f, 1.85f}, {0.46f, 1.05f, 3.4f}};   // E2M1, E4M3, widened
     constexpr float ENDS_US[3] = {0.7f, 2.2f, 3.5f};
     const float* const us = STAGE_US[four ? 0 : p.f32 ? 2 : 1];
     const int stages = (p.K + (four ? 255 : 127)) / (four ? 256 : 128);
@@ -498,14 +504,14 @@ static MxPlan plan(const MxProduct& p) {
     return best;
 }
 
-template <int FA, int FB, bool WIDE, typename TC, int BM, int BN, int WR, int WC, int NS>
+template <int FA, int FB, bool WIDE, typename TC, int KS, int BM, int BN, int WR, int WC, int NS>
 static hipError_t launch_tiles(const MxProduct& q, int split, void* ws, hipStream_t st) {
-    constexpr int KS = STAGE_K<FA, FB>, NW = WR * WC;
+    constexpr int NW = WR * WC;
     using A = MxTile<FA, KS, BM, NW>;
     using B = MxTile<FB, KS, BN, NW>;
     constexpr int LDS = std::max(NS * (A::BYTES + B::BYTES + A::SCALES + B::SCALES), NW * 4096);
     static std::atomic<uint64_t> lds_ok{0};
-    auto kern = &k_product_tiles<FA, FB, WIDE, TC, BM, BN, WR, WC, NS>;
+    auto kern = &k_product_tiles<FA, FB, WIDE, TC, KS, BM, BN, WR, WC, NS>;
     const hipError_t e = allow_lds((const void*)kern, LDS, lds_ok);
     if (e != hipSuccess) return e;
     const long width = mx_width(q.K);
@@ -554,17 +560,19 @@ template <int FA, int FB, bool WIDE, typename TC>
 static hipError_t run_product(const MxProduct& p, void* ws, hipStream_t st) {
     // Stages: three hide a request's way where LDS has room for them, which it has where one side is half the bytes (4096x8192x12288 E4M3 by
     // E2M1 322 -> 306 us), for tiles of 64 (four are 2 % slower, two up to 30 %), and for one workgroup of tiles of 128 on a compute unit
-    // (2048x2048x8192 E4M3 57.4 -> 45.0), where a second one does so too (2048x4096x4096, two of them: 47.7, one at a time 50.3).
-    constexpr int NS = FA == FB ? 2 : 3;
+    // (2048x2048x8192 E4M3 57.4 -> 45.0), where a second one does so too (2048x4096x4096, two of them: 47.7, one at a time 50.3).  Tiles of 64
+    // that are widened do better with two stages of 256 k, half as many ends of one (1024x1024x4096 18.5 -> 16.3 us, 1003x700x2050 11.2 -> 10.4);
+    // the others do not (11.2 and 12.1, 7.3 and 7.9).
+    constexpr int NS = FA == FB ? 2 : 3, KS = STAGE_K<FA, FB>;
     const MxPlan l = plan(p);
     switch (l.kernel) {
         case ROWS_16: return launch_rows<FA, FB, WIDE, TC, 1>(p, st);
         case ROWS_32: return launch_rows<FA, FB, WIDE, TC, 2>(p, st);
-        case TILES_64: return launch_tiles<FA, FB, WIDE, TC, 64, 64, 2, 2, 3>(p, l.split, ws, st);
+        case TILES_64: return launch_tiles<FA, FB, WIDE, TC, WIDE ? 256 : KS, 64, 64, 2, 2, WIDE ? 2 : 3>(p, l.split, ws, st);
         case TILES_128:
-            if (NS == 3 || tiles_of(p, 128) * l.split <= CUS) return launch_tiles<FA, FB, WIDE, TC, 128, 128, 2, 2, 3>(p, l.split, ws, st);
-            return launch_tiles<FA, FB, WIDE, TC, 128, 128, 2, 2, 2>(p, l.split, ws, st);
-        default: return launch_tiles<FA, FB, WIDE, TC, 256, 256, 2, 4, NS>(p, l.split, ws, st);
+            if (NS == 3 || tiles_of(p, 128) * l.split <= CUS) return launch_tiles<FA, FB, WIDE, TC, KS, 128, 128, 2, 2, 3>(p, l.split, ws, st);
+            return launch_tiles<FA, FB, WIDE, TC, KS, 128, 128, 2, 2, 2>(p, l.split, ws, st);
+        default: return launch_tiles<FA, FB, WIDE, TC, KS, 256, 256, 2, 4, NS>(p, l.split, ws, st);
     }
 }
 hipError_t mx_product(const MxProduct& p, void* ws, hipStream_t st) {

@@ -478,7 +478,7 @@ def test_product_adds_to_what_is_there(ctx, dtype, fa, fb):
 
 
 @pytest.mark.parametrize("fa,fb", PAIRS)
-@pytest.mark.parametrize("m,n,k", [(256, 512, 2048), (1024, 768, 1280), (2047, 1030, 900), (700, 5000, 4100), (3000, 2900, 700), (970, 1106, 5422), (1106, 4096, 7424)])
+@pytest.mark.parametrize("m,n,k", [(256, 512, 2048), (1024, 768, 1280), (2047, 1030, 900), (700, 5000, 4100), (3000, 2900, 700), (970, 1106, 3328), (1106, 4096, 7424), (1500, 2696, 8448)])
 def test_larger_products(ctx, m, n, k, fa, fb):
     for dtype in ("bf16", "f32"):
         check_product(ctx, m, n, k, fa, fb, dtype)
