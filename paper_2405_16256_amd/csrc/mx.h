@@ -170,42 +170,129 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t magnitude) {
     const int e = (int)(magnitude >> 23);
     return e == 255 ? 255u : (uint32_t)max(e - Mx<F>::TOP, 0);
 }
-// What a block's values are multiplied by: one over its scale, exactly.
-__device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 // A scale as a number: 2^(byte - 127), NaN for 255
 __device__ __forceinline__ float scale_value(uint32_t byte) {
     return __uint_as_float(byte == 255u ? 0x7FC00000u : byte ? byte << 23 : 0x00400000u);
 }
-// Eight values, multiplied by `inv`, as codes in memory order.  The conversions round to nearest, ties to even; the one to four bits
-// saturates by itself, the one to eight makes a NaN of what rounds past 448.
-__device__ __forceinline__ uint32_t codes_e2m1(const float* v, float inv) {
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0] * inv, v[1] * inv, 1.f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2] * inv, v[3] * inv, 1.f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * inv, v[5] * inv, 1.f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * inv, v[7] * inv, 1.f, 3);
-    return c;
-}
-__device__ __forceinline__ uint32_t codes_e4m3(float a, float b, float c, float d, float inv) {
-    auto clamp = [](float x) { return __builtin_amdgcn_fmed3f(x, -448.f, 448.f); };
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(clamp(a * inv), clamp(b * inv), 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp(c * inv), clamp(d * inv), r, true);
-}
-constexpr uint32_t NAN_CODES_E2M1 = 0x77777777u, NAN_CODES_E4M3 = 0x7F7F7F7Fu;   // any value times the scale NaN
-template <int F> struct Codes8;   // eight codes as they lie in memory
-template <> struct Codes8<MX_E4M3> {
-    uint2 w;
-    __device__ __forceinline__ void set(const float* v, uint32_t byte) {
-        const float inv = scale_inverse(byte);
-        w = byte == 255u ? make_uint2(NAN_CODES_E4M3, NAN_CODES_E4M3)
-                         : make_uint2(codes_e4m3(v[0], v[1], v[2], v[3], inv), codes_e4m3(v[4], v[5], v[6], v[7], inv));
-    }
-    __device__ __forceinline__ void store(uint8_t* row, size_t chunk) const { *reinterpret_cast<uint2*>(row + 8 * chunk) = w; }
-};
-template <> struct Codes8<MX_E2M1> {
+// Two neighbouring values of a block, as the conversions take them
+template <typename T> struct Pair;
+template <> struct Pair<float> { float a, b; };
+template <> struct Pair<bf16_t> {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     uint32_t w;
-    __device__ __forceinline__ void set(const float* v, uint32_t byte) { w = byte == 255u ? NAN_CODES_E2M1 : codes_e2m1(v, scale_inverse(byte)); }
-    __device__ __forceinline__ void store(uint8_t* row, size_t chunk) const { *reinterpret_cast<uint32_t*>(row + 4 * chunk) = w; }
+};
+// Codes of a block's values.  The conversions divide by the scale, of which they take the exponent alone (0 is 2^-127), and round once, to
+// nearest, ties to even.  The ones to four bits saturate by themselves, those to eight make a NaN of what rounds past 448.
+template <int F>
+struct Packer {
+    uint32_t byte;
+    __device__ __forceinline__ explicit Packer(uint32_t magnitude) : byte(scale_byte<F>(magnitude)) {}
+    __device__ __forceinline__ float scale() const { return __uint_as_float(byte << 23); }
+    // `into` with the codes of a pair in byte (E4M3: half word) AT
+    template <int AT> __device__ __forceinline__ uint32_t put(uint32_t into, Pair<float> p) const {
+        if constexpr (F == MX_E2M1) return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(into, p.a, p.b, scale(), AT);
+        else {
+            const float inv = __uint_as_float((254u - byte) << 23);
+            return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_fmed3f(p.a * inv, -448.f, 448.f),
+                                                             __builtin_amdgcn_fmed3f(p.b * inv, -448.f, 448.f), (int)into, AT == 1);
+        }
+    }
+    template <int AT> __device__ __forceinline__ uint32_t put(uint32_t into, Pair<bf16_t> p) const {
+        Pair<bf16_t>::bf16x2 v;
+        if constexpr (F == MX_E2M1) {
+            __builtin_memcpy(&v, &p.w, 4);
+            return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(into, v, scale(), AT);
+        } else {   // 448 times the scale: the magnitudes' bits are in the order of the numbers
+            const uint16_t most = (uint16_t)((byte + 8u) << 7 | 0x60u);
+            typedef short s16x2 __attribute__((ext_vector_type(2)));
+            Pair<bf16_t>::u16x2 m;
+            s16x2 c;
+            const uint32_t magnitudes = p.w & 0x7FFF7FFFu;
+            __builtin_memcpy(&m, &magnitudes, 4);
+            m = __builtin_elementwise_min(m, Pair<bf16_t>::u16x2{most, most});
+            uint32_t w;
+            __builtin_memcpy(&w, &m, 4);
+            w |= p.w & 0x80008000u;
+            __builtin_memcpy(&v, &w, 4);
+            __builtin_memcpy(&c, &into, 4);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, v, scale(), AT == 1);
+            __builtin_memcpy(&into, &c, 4);
+            return into;
+        }
+    }
+    // A block that holds a NaN or an infinity: any value times the scale NaN
+    __device__ __forceinline__ uint32_t checked(uint32_t codes) const { return byte != 255u ? codes : F == MX_E2M1 ? 0x77777777u : 0x7F7F7F7Fu; }
+    template <typename T> __device__ __forceinline__ uint32_t four(Pair<T> p, Pair<T> q) const { return checked(put<1>(put<0>(0u, p), q)); }   // E2M1: 16 bits of it
+    // Eight values as they lie in memory
+    template <typename T> __device__ __forceinline__ void eight(const Pair<T>* p, uint32_t* to) const {
+        if constexpr (F == MX_E2M1) to[0] = checked(put<3>(put<2>(put<1>(put<0>(0u, p[0]), p[1]), p[2]), p[3]));
+        else {
+            to[0] = four(p[0], p[1]);
+            to[1] = four(p[2], p[3]);
+        }
+    }
+    template <typename T> __device__ __forceinline__ void store8(const Pair<T>* p, uint8_t* row, size_t chunk) const {
+        uint32_t w[2];
+        eight(p, w);
+        if constexpr (F == MX_E2M1) *reinterpret_cast<uint32_t*>(row + 4 * chunk) = w[0];
+        else *reinterpret_cast<uint2*>(row + 8 * chunk) = make_uint2(w[0], w[1]);
+    }
+};
+template <int N> __device__ __forceinline__ Pair<bf16_t> pair_of(const Few<bf16_t, N>& v, int i) { return {v.w[i]}; }   // values 2 i, 2 i + 1
+template <int N> __device__ __forceinline__ Pair<float> pair_of(const Few<float, N>& v, int i) { return {v.at(2 * i), v.at(2 * i + 1)}; }
+// Value j of a and of b
+template <int N> __device__ __forceinline__ Pair<bf16_t> pair_across(const Few<bf16_t, N>& a, const Few<bf16_t, N>& b, int j) {
+    return {__builtin_amdgcn_perm(b.w[j >> 1], a.w[j >> 1], j & 1 ? 0x07060302u : 0x05040100u)};
+}
+template <int N> __device__ __forceinline__ Pair<float> pair_across(const Few<float, N>& a, const Few<float, N>& b, int j) { return {a.at(j), b.at(j)}; }
+
+// Magnitudes of N values as they lie in memory, two bf16 to a word: their order as integers is that of the numbers, and two are compared at
+// a time.
+template <typename T, int N> struct Magnitudes;
+template <int N> struct Magnitudes<bf16_t, N> {
+    uint32_t w[N / 2];
+    __device__ __forceinline__ static uint32_t larger(uint32_t a, uint32_t b) {
+        Pair<bf16_t>::u16x2 x, y;
+        __builtin_memcpy(&x, &a, 4);
+        __builtin_memcpy(&y, &b, 4);
+        x = __builtin_elementwise_max(x, y);
+        __builtin_memcpy(&a, &x, 4);
+        return a;
+    }
+    __device__ __forceinline__ explicit Magnitudes(const Few<bf16_t, N>& v) {
+#pragma unroll
+        for (int i = 0; i < N / 2; i++) w[i] = v.w[i] & 0x7FFF7FFFu;
+    }
+    __device__ __forceinline__ void add(const Magnitudes& o) {
+#pragma unroll
+        for (int i = 0; i < N / 2; i++) w[i] = larger(w[i], o.w[i]);
+    }
+    __device__ __forceinline__ uint32_t column(int j) const { return (j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xFFFFu) << 16; }   // as of fp32
+    __device__ __forceinline__ uint32_t largest() const {
+        uint32_t m = w[0];
+#pragma unroll
+        for (int i = 1; i < N / 2; i++) m = larger(m, w[i]);
+        return max(m >> 16, m & 0xFFFFu) << 16;
+    }
+};
+template <int N> struct Magnitudes<float, N> {
+    uint32_t w[N];
+    __device__ __forceinline__ explicit Magnitudes(const Few<float, N>& v) {
+#pragma unroll
+        for (int i = 0; i < N; i++) w[i] = v.w[i >> 2][i & 3] & 0x7FFFFFFFu;
+    }
+    __device__ __forceinline__ void add(const Magnitudes& o) {
+#pragma unroll
+        for (int i = 0; i < N; i++) w[i] = max(w[i], o.w[i]);
+    }
+    __device__ __forceinline__ uint32_t column(int j) const { return w[j]; }
+    __device__ __forceinline__ uint32_t largest() const {
+        uint32_t m = w[0];
+#pragma unroll
+        for (int i = 1; i < N; i++) m = max(m, w[i]);
+        return m;
+    }
 };
 // The largest of a value over the four neighbouring lanes that share a block
 __device__ __forceinline__ uint32_t quad_max(uint32_t m) {

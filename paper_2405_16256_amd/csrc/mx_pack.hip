@@ -19,62 +19,31 @@ __global__ __launch_bounds__(256) void k_pack_rows(int chunks, Divisor per_row, 
     const int group = split_off(row, per_row), n = cols - 8 * group;
     Eight<T> e{};
     if (n > 0) e.template load<STREAM>(x + row * ldx + 8L * group, n);
-    float v[8];
-    e.widen(v);
-    const uint32_t byte = scale_byte<F>(quad_max(magnitude8(v)));
-    Codes8<F> q;
-    q.set(v, byte);
-    q.store(codes, (size_t)i);
-    if ((group & 3) == 0) scales[(size_t)i >> 2] = (uint8_t)byte;
+    const Packer<F> q(quad_max(Magnitudes<T, 8>(e).largest()));
+    const Pair<T> pairs[4] = {pair_of(e, 0), pair_of(e, 1), pair_of(e, 2), pair_of(e, 3)};
+    q.store8(pairs, codes, (size_t)i);
+    if ((group & 3) == 0) scales[(size_t)i >> 2] = (uint8_t)q.byte;
 }
 
-// Magnitudes of four columns as they lie in memory, two bf16 to a word: their order as integers is that of the numbers, and two are compared at
-// a time.
-template <typename T> struct Magnitudes;
-template <> struct Magnitudes<bf16_t> {
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    uint32_t w[2];
-    __device__ __forceinline__ static uint32_t larger(uint32_t a, uint32_t b) {
-        u16x2 x, y;
-        __builtin_memcpy(&x, &a, 4);
-        __builtin_memcpy(&y, &b, 4);
-        x = __builtin_elementwise_max(x, y);
-        __builtin_memcpy(&a, &x, 4);
-        return a;
-    }
-    __device__ __forceinline__ explicit Magnitudes(const Few<bf16_t, 4>& v) : w{v.w[0] & 0x7FFF7FFFu, v.w[1] & 0x7FFF7FFFu} {}
-    __device__ __forceinline__ void add(const Magnitudes& o) { w[0] = larger(w[0], o.w[0]); w[1] = larger(w[1], o.w[1]); }
-    __device__ __forceinline__ uint32_t column(int j) const { return (j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xFFFFu) << 16; }   // as of fp32
-    __device__ __forceinline__ uint32_t largest() const { const uint32_t m = larger(w[0], w[1]); return max(m >> 16, m & 0xFFFFu) << 16; }
-};
-template <> struct Magnitudes<float> {
-    uint32_t w[4];
-    __device__ __forceinline__ explicit Magnitudes(const Few<float, 4>& v) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) w[i] = v.w[0][i] & 0x7FFFFFFFu;
-    }
-    __device__ __forceinline__ void add(const Magnitudes& o) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) w[i] = max(w[i], o.w[i]);
-    }
-    __device__ __forceinline__ uint32_t column(int j) const { return w[j]; }
-    __device__ __forceinline__ uint32_t largest() const { return max(max(w[0], w[1]), max(w[2], w[3])); }
-};
-
 // ------------------------------------------------------------------ by column, and both
-// A lane takes 4 columns of a block of 32 rows in registers, ACROSS lanes the columns beside them and 64 / ACROSS the row blocks below: blocks
-// along columns need no exchange at all, those along rows one of eight lanes, and x is read once for both.  11008x4096 bf16 to E2M1 both
-// ways 38.8 us from memory (3.6 TB/s; 34 without the rows' codes, of which a lane has two bytes), packing twice 46.
-template <typename T, int F, bool ROWS, int ACROSS, bool STREAM>
+// A workgroup takes 256 rows x 128 columns, a lane 4 columns of a block of 32 rows in registers: blocks along columns need no exchange at all,
+// those along rows one of eight lanes, and x is read once for both.  Codes and scales go out through LDS, whole lines at a time.
+constexpr int PACK_ROWS = 256, PACK_COLS = 128;
+template <typename T, int F, bool ROWS, bool STREAM>
 __global__ __launch_bounds__(256) void k_pack_columns(long rows, int cols, const T* __restrict__ x, long ldx, int width, uint8_t* __restrict__ codes,
                                                        uint8_t* __restrict__ scales, long column_width, uint8_t* __restrict__ column_codes,
-                                                       uint8_t* __restrict__ column_scales, Divisor tiles_across) {
-    constexpr int BITS = F == MX_E4M3 ? 8 : 4, DOWN = 64 / ACROSS;
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    int down = (int)blockIdx.x;
-    const int across = split_off(down, tiles_across);
-    const int col0 = (across * 4 + wave) * (4 * ACROSS) + (lane % ACROSS) * 4;
-    const long block = (long)down * DOWN + lane / ACROSS, row0 = block * 32;
+                                                       uint8_t* __restrict__ column_scales, Divisor tiles_in_line) {
+    constexpr int BITS = F == MX_E4M3 ? 8 : 4, CODES = PACK_ROWS * PACK_COLS * BITS / 8, ROW = PACK_COLS * BITS / 8, COLUMN = PACK_ROWS * BITS / 8;
+    constexpr int CHUNKS = COLUMN / 16;   // of a column in LDS, turned by it
+    __shared__ __attribute__((aligned(16))) uint8_t smem[CODES + PACK_ROWS * PACK_COLS / MX_BLOCK];
+    const int t = (int)threadIdx.x, lane = t & 63, block = 2 * (t >> 6) + (lane >> 5), c = 4 * (lane & 31);
+    // Each die takes a run of tiles (workgroups go to the eight of them in turn), so that the tiles that share a line of what is written meet
+    // in one L2.
+    const int run = (int)gridDim.x >> 3, b = (int)blockIdx.x;
+    int line = b < 8 * run ? (b & 7) * run + (b >> 3) : b;
+    const int place = split_off(line, tiles_in_line), across = ROWS ? place : line, down = ROWS ? line : place;
+    const int tile_col = across * PACK_COLS, col0 = tile_col + c;
+    const long tile_row = (long)down * PACK_ROWS, row0 = tile_row + 32 * block;
     const int n = cols - col0, there = (int)min(rows - row0, 32L);   // rows of the block; none of a block of padding
     const T* const from = x + row0 * ldx + col0;
     Few<T, 4> raw[32];
@@ -88,53 +57,64 @@ __global__ __launch_bounds__(256) void k_pack_columns(long rows, int cols, const
             if (n > 0 && r < there) raw[r].template load<STREAM>(from + r * ldx, n);
         }
     }
-    Magnitudes<T> most(raw[0]);
-#pragma unroll
-    for (int r = 1; r < 32; r++) most.add(Magnitudes<T>(raw[r]));
-    if (ROWS && col0 < width) {
-        uint8_t* to = codes + ((size_t)row0 * width + col0) * BITS / 8;
-        uint8_t* scale = scales + (size_t)row0 * (width / MX_BLOCK) + (col0 >> 5);
+    if (ROWS) {
 #pragma unroll
         for (int r = 0; r < 32; r++) {
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = i < 4 ? raw[r].at(i) : 0.f;
-            uint32_t m = quad_max(magnitude8(v));
+            uint32_t m = quad_max(Magnitudes<T, 4>(raw[r]).largest());
             m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xF, 0xF, true));   // the other four of eight lanes
-            const uint32_t byte = scale_byte<F>(m);
-            Codes8<F> q;
-            q.set(v, byte);
-            if (r < there) {
-                if constexpr (F == MX_E4M3) *reinterpret_cast<uint32_t*>(to) = q.w.x;
-                else *reinterpret_cast<uint16_t*>(to) = (uint16_t)q.w;
-                if ((col0 & 31) == 0) *scale = (uint8_t)byte;
-            }
-            to += (size_t)width * BITS / 8;
-            scale += width / MX_BLOCK;
+            const Packer<F> q(m);
+            const uint32_t w = q.four(pair_of(raw[r], 0), pair_of(raw[r], 1));
+            uint8_t* const to = smem + (32 * block + r) * ROW + c * BITS / 8;
+            if constexpr (F == MX_E4M3) *reinterpret_cast<uint32_t*>(to) = w;
+            else *reinterpret_cast<uint16_t*>(to) = (uint16_t)w;
+            if ((lane & 7) == 0) smem[CODES + (32 * block + r) * (PACK_COLS / MX_BLOCK) + c / MX_BLOCK] = (uint8_t)q.byte;
         }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ROW / 16; i++) {
+            const int at = i * 256 + t, r = at / (ROW / 16), piece = at % (ROW / 16);
+            if (tile_row + r < rows)
+                *reinterpret_cast<uint4*>(codes + ((size_t)(tile_row + r) * width * BITS / 8) + (tile_col * BITS / 8 + 16 * piece)) =
+                    reinterpret_cast<const uint4*>(smem)[at];
+        }
+        if (tile_row + t < rows)
+            *reinterpret_cast<uint32_t*>(scales + (size_t)(tile_row + t) * (width / MX_BLOCK) + tile_col / MX_BLOCK) =
+                reinterpret_cast<const uint32_t*>(smem + CODES)[t];
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 32; r++) raw[r].hide();   // what was derived from them is formed again: half the registers
     }
+    Magnitudes<T, 4> most(raw[0]);
+#pragma unroll
+    for (int r = 1; r < 32; r++) most.add(Magnitudes<T, 4>(raw[r]));
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-        if (j >= n) continue;
-        const uint32_t byte = scale_byte<F>(most.column(j));
+        const Packer<F> q(most.column(j));
         uint32_t w[BITS];   // 32 codes
 #pragma unroll
         for (int k = 0; k < 4; k++) {
-            float v[8];
+            Pair<T> pairs[4];
 #pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = raw[8 * k + i].at(j);
-            Codes8<F> q;
-            q.set(v, byte);
-            if constexpr (F == MX_E4M3) { w[2 * k] = q.w.x; w[2 * k + 1] = q.w.y; }
-            else w[k] = q.w;
+            for (int i = 0; i < 4; i++) pairs[i] = pair_across(raw[8 * k + 2 * i], raw[8 * k + 2 * i + 1], j);
+            q.eight(pairs, w + k * BITS / 4);
         }
-        uint4* const to = reinterpret_cast<uint4*>(column_codes + ((size_t)(col0 + j) * column_width + row0) * BITS / 8);
-        if (row0 < column_width) {
-            to[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            if constexpr (BITS == 8) to[1] = make_uint4(w[4], w[5], w[6], w[7]);
-            column_scales[(size_t)(col0 + j) * (column_width / MX_BLOCK) + block] = (uint8_t)byte;
-        }
+#pragma unroll
+        for (int i = 0; i < BITS / 4; i++)
+            *reinterpret_cast<uint4*>(smem + (c + j) * COLUMN + 16 * ((block * (BITS / 4) + i) ^ (c / 4 & (CHUNKS - 1)))) =
+                make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        smem[CODES + (c + j) * (PACK_ROWS / MX_BLOCK) + block] = (uint8_t)q.byte;
     }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < COLUMN * PACK_COLS / 4096; i++) {
+        const int at = i * 256 + t, col = at / CHUNKS, piece = (at % CHUNKS) ^ (col / 4 & (CHUNKS - 1));
+        if (tile_col + col < cols)
+            *reinterpret_cast<uint4*>(column_codes + ((size_t)(tile_col + col) * column_width * BITS / 8) + (tile_row * BITS / 8 + 16 * piece)) =
+                reinterpret_cast<const uint4*>(smem)[at];
+    }
+    if (t < PACK_COLS && tile_col + t < cols)
+        *reinterpret_cast<uint2*>(column_scales + (size_t)(tile_col + t) * (column_width / MX_BLOCK) + tile_row / MX_BLOCK) =
+            reinterpret_cast<const uint2*>(smem + CODES)[t];
 }
 
 template <typename T, int F>
@@ -148,17 +128,14 @@ static hipError_t quantise(long rows, long cols, const void* x, long ldx, const 
         return hipGetLastError();
     }
     const long column_width = mx_width(rows);
-    // Wide tiles where rows are written too, tall ones where columns alone are: 11008x4096 bf16 to E2M1, past the caches, both ways with 16, 32
-    // and 64 lanes across 41.7, 38.8 and 45.6 us, by column alone 24.7, 28.1 and 39.9.
-    auto tiles = [&](auto kern, int lanes) {
-        const int across = ((by_row.codes ? width : (int)cols) + 16 * lanes - 1) / (16 * lanes);
-        const unsigned grid = (unsigned)(across * ((column_width + 2048 / lanes - 1) / (2048 / lanes)));
-        kern<<<grid, 256, 0, st>>>(rows, (int)cols, (const T*)x, ldx, width, by_row.codes, by_row.scales, column_width, by_column.codes, by_column.scales,
-                                   divisor(across));
+    const int across = by_row.codes ? width / PACK_COLS : ((int)cols + PACK_COLS - 1) / PACK_COLS, down = (int)(column_width / PACK_ROWS);
+    auto run = [&](auto kern) {
+        kern<<<(unsigned)(across * down), 256, 0, st>>>(rows, (int)cols, (const T*)x, ldx, width, by_row.codes, by_row.scales, column_width, by_column.codes,
+                                                        by_column.scales, divisor(by_row.codes ? across : down));
         return hipGetLastError();
     };
-    if (by_row.codes) return tiles(stream ? &k_pack_columns<T, F, true, 32, true> : &k_pack_columns<T, F, true, 32, false>, 32);
-    return tiles(stream ? &k_pack_columns<T, F, false, 16, true> : &k_pack_columns<T, F, false, 16, false>, 16);
+    if (by_row.codes) return run(stream ? &k_pack_columns<T, F, true, true> : &k_pack_columns<T, F, true, false>);
+    return run(stream ? &k_pack_columns<T, F, false, true> : &k_pack_columns<T, F, false, false>);
 }
 hipError_t mx_quantise(int dtype, long rows, long cols, const void* x, long ldx, int format, const MxRows& by_row, const MxRows& by_column,
                        hipStream_t st) {

@@ -118,15 +118,16 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
         }
         if (format != MX_NONE && 8 * group < width) {   // whole blocks of 32: the four lanes of one are here together
             const uint32_t m = quad_max(magnitude8(u));
+            const Pair<float> pairs[4] = {{u[0], u[1]}, {u[2], u[3]}, {u[4], u[5]}, {u[6], u[7]}};
             uint32_t byte;
             if (format == MX_E4M3) {
-                Codes8<MX_E4M3> q;
-                q.set(u, byte = scale_byte<MX_E4M3>(m));
-                q.store(codes + (size_t)row * width, group);
+                const Packer<MX_E4M3> q(m);
+                byte = q.byte;
+                q.store8(pairs, codes + (size_t)row * width, group);
             } else {
-                Codes8<MX_E2M1> q;
-                q.set(u, byte = scale_byte<MX_E2M1>(m));
-                q.store(codes + (size_t)row * (width / 2), group);
+                const Packer<MX_E2M1> q(m);
+                byte = q.byte;
+                q.store8(pairs, codes + (size_t)row * (width / 2), group);
             }
             if ((group & 3) == 0) scales[(size_t)row * (width / MX_BLOCK) + (group >> 2)] = (uint8_t)byte;
         }
