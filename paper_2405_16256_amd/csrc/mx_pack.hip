@@ -5,29 +5,44 @@
 
 namespace hh {
 
-// Packing.  A block's scale is the exponent of its largest magnitude, which is compared as an integer, and every value is multiplied by one
-// over the scale, exactly, before it is rounded: one read, one pass, no division.  Bound by memory.
+// Packing.  A block's scale is the exponent of its largest magnitude, which is compared as an integer, and the conversions take values as they lie
+// in memory, two at a time, with the scale: one read, one pass, one rounding.  Bound by memory.
 
 // ------------------------------------------------------------------ by row
-// Eight values a lane, four lanes a block.  11008x4096 bf16 to E2M1 18.9 us from the last-level cache (6.0 TB/s), 21.3 from memory.
+// Eight values a lane, four lanes a block; past the caches two such chunks a lane, with both loads under way, and codes that go past them too:
+// 11008x4096 bf16 to E2M1 18.5 us (6.1 TB/s; one chunk 21.0, stores through the caches 19.3, both 22.7), to E4M3 22.4 (26.0).  Small tensors
+// lose by the second chunk (333x2050 2.3 -> 2.6).
+template <bool STREAM> constexpr int chunks_each() { return STREAM ? 2 : 1; }
 template <typename T, int F, bool STREAM>
 __global__ __launch_bounds__(256) void k_pack_rows(int chunks, Divisor per_row, int cols, const T* __restrict__ x, long ldx, uint8_t* __restrict__ codes,
                                                     uint8_t* __restrict__ scales) {
-    const int i = (int)(blockIdx.x * 256u + threadIdx.x);
-    if (i >= chunks) return;   // whole rows of a multiple of 32 chunks
-    int row = i;
-    const int group = split_off(row, per_row), n = cols - 8 * group;
-    Eight<T> e{};
-    if (n > 0) e.template load<STREAM>(x + row * ldx + 8L * group, n);
-    const Packer<F> q(quad_max(Magnitudes<T, 8>(e).largest()));
-    const Pair<T> pairs[4] = {pair_of(e, 0), pair_of(e, 1), pair_of(e, 2), pair_of(e, 3)};
-    q.store8(pairs, codes, (size_t)i);
-    if ((group & 3) == 0) scales[(size_t)i >> 2] = (uint8_t)q.byte;
+    constexpr int EACH = chunks_each<STREAM>();
+    const unsigned first = blockIdx.x * (256u * EACH) + threadIdx.x;
+    Eight<T> e[EACH];
+#pragma unroll
+    for (int c = 0; c < EACH; c++) {
+        e[c] = Eight<T>{};
+        if (first + 256u * c >= (unsigned)chunks) continue;   // whole rows of a multiple of 32 chunks
+        int row = (int)(first + 256u * c);
+        const int group = split_off(row, per_row), n = cols - 8 * group;
+        if (n > 0) e[c].template load<STREAM>(x + row * ldx + 8L * group, n);
+    }
+#pragma unroll
+    for (int c = 0; c < EACH; c++) {
+        const unsigned i = first + 256u * c;
+        if (i >= (unsigned)chunks) return;
+        const Packer<F> q(quad_max(Magnitudes<T, 8>(e[c]).largest()));
+        const Pair<T> pairs[4] = {pair_of(e[c], 0), pair_of(e[c], 1), pair_of(e[c], 2), pair_of(e[c], 3)};
+        q.template store8<STREAM>(pairs, codes, i);
+        store_scales(scales + (i >> 2), q.byte);
+    }
 }
 
 // ------------------------------------------------------------------ by column, and both
 // A workgroup takes 256 rows x 128 columns, a lane 4 columns of a block of 32 rows in registers: blocks along columns need no exchange at all,
 // those along rows one of eight lanes, and x is read once for both.  Codes and scales go out through LDS, whole lines at a time.
+// 11008x4096 bf16 from memory, both ways, to E2M1 32.3 us (4.3 TB/s; 35.8 straight from registers, 16 and 2 bytes a lane; packing twice 43), to E4M3
+// 40.9; by column alone 21.6 and 26.2.  Without any store it is 22, of which the rows' part of the arithmetic is 8.
 constexpr int PACK_ROWS = 256, PACK_COLS = 128;
 template <typename T, int F, bool ROWS, bool STREAM>
 __global__ __launch_bounds__(256) void k_pack_columns(long rows, int cols, const T* __restrict__ x, long ldx, int width, uint8_t* __restrict__ codes,
@@ -124,7 +139,8 @@ static hipError_t quantise(long rows, long cols, const void* x, long ldx, const 
     if (!by_column.codes) {
         const int chunks = (int)(rows * (width / 8));
         auto kern = stream ? &k_pack_rows<T, F, true> : &k_pack_rows<T, F, false>;
-        kern<<<((unsigned)chunks + 255u) / 256u, 256, 0, st>>>(chunks, divisor(width / 8), (int)cols, (const T*)x, ldx, by_row.codes, by_row.scales);
+        const unsigned each = 256u * (stream ? chunks_each<true>() : chunks_each<false>());
+        kern<<<((unsigned)chunks + each - 1) / each, 256, 0, st>>>(chunks, divisor(width / 8), (int)cols, (const T*)x, ldx, by_row.codes, by_row.scales);
         return hipGetLastError();
     }
     const long column_width = mx_width(rows);
@@ -147,7 +163,7 @@ hipError_t mx_quantise(int dtype, long rows, long cols, const void* x, long ldx,
 }
 
 // ------------------------------------------------------------------ values
-// 4096x11008 of E2M1 to bf16 16.9 us (6.7 TB/s).
+// 4096x11008 of E2M1 to bf16 16.9 us (6.7 TB/s), 8192x8192 of E4M3 to fp32 60 (5.7).
 template <typename T, int F, bool STREAM>
 __global__ __launch_bounds__(256) void k_values(int chunks, Divisor per_row, int k, int width, const uint8_t* __restrict__ codes,
                                                  const uint8_t* __restrict__ scales, T* __restrict__ y, long ldy) {

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
                 byte = q.byte;
                 q.store8(pairs, codes + (size_t)row * (width / 2), group);
             }
-            if ((group & 3) == 0) scales[(size_t)row * (width / MX_BLOCK) + (group >> 2)] = (uint8_t)byte;
+            store_scales(scales + (size_t)row * (width / MX_BLOCK) + (group >> 2), byte);
         }
     }
 }

@@ -228,6 +228,23 @@ def test_every_number_border_and_tie(ctx, fmt):
 
 @pytest.mark.parametrize("fmt", ("e4m3", "e2m1"))
 @pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_every_exponent_of_a_block(ctx, fmt, dtype):
+    """Blocks of bf16 bit patterns: the largest of every exponent there is, the others up to 20 powers of two below it."""
+    rng = np.random.default_rng(8)
+    top = np.repeat(np.arange(255), 16)[:, None]
+    bits = np.maximum(top - rng.integers(0, 21, (len(top), 32)), 0) << 7 | rng.integers(0, 128, (len(top), 32)) | rng.integers(0, 2, (len(top), 32)) << 15
+    bits[np.arange(len(top)), rng.integers(0, 32, len(top))] = top[:, 0] << 7 | rng.integers(0, 128, len(top))
+    x = (bits.astype(np.uint32) << 16).view(np.float32)
+    t = torch.from_numpy(x).to(TYPES[dtype][0])
+    for rows, cols, src in ((len(x), 32, t), (32, len(x), t.t().contiguous())):
+        q, c = Packed(rows, cols, fmt), Packed(cols, rows, fmt)
+        hh.hh_mx_quantise(ctx, rows, cols, TYPES[dtype][1], src.to(L.DEV), cols, FORMATS[fmt][1], q.struct, c.struct, L.stream_ptr())
+        check_packed(q, src.double().numpy(), "row")
+        check_packed(c, src.double().numpy().T, "column")
+
+
+@pytest.mark.parametrize("fmt", ("e4m3", "e2m1"))
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
 def test_smallest_largest_and_what_is_no_number(ctx, fmt, dtype):
     big = 3.3895313892515355e38                                 # the largest bf16
     x = np.zeros((8, 64), dtype=np.float32)
