@@ -11,8 +11,8 @@ namespace hh {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));   // a bfloat16's alignment
 // STREAM: the launch reads and writes more than the last-level cache keeps for the next one anyway (STREAM_BYTES).  Past the caches, cold
-// tensors: dropout of 4096x12288 bf16 39.1 -> 36.6 us, residual addition with norm and packing 117 -> 105, 11008x4096 packed both ways
-// and unpacked 88 -> 78.  Smaller ones are read by what follows while they are there.
+// tensors: dropout of 4096x12288 bf16 39.1 -> 36.6 us, residual addition with norm and packing 117 -> 105.  Smaller ones are read by what
+// follows while they are there.
 constexpr double STREAM_BYTES = 96e6;
 template <bool STREAM, typename V>
 __device__ __forceinline__ V load_any(const V* p) { return STREAM ? __builtin_nontemporal_load(p) : *p; }
