@@ -409,8 +409,8 @@ def _nearest(x, format):
     powers = torch.tensor([2.0 ** e for e in range(-126 + top, 128)], dtype=torch.float64, device=DEVICE)
     pieces = torch.split(x, BLOCK, dim=1)
     full = torch.nn.utils.rnn.pad_sequence([p.t() for p in pieces], batch_first=True) if x.shape[1] % BLOCK else torch.stack([p.t() for p in pieces])
-    reached = torch.bucketize(full.abs().amax(dim=1), powers, right=True)   # blocks x rows: powers of two at or below the largest
-    scale = torch.tensor([2.0 ** (i - 127) for i in range(len(powers) + 1)], dtype=torch.float64, device=DEVICE)[reached][:, None, :]
+    scale = torch.bucketize(full.abs().amax(dim=1), powers, right=True)   # blocks x rows: powers of two at or below the largest
+    scale = torch.pow(torch.tensor(2.0, dtype=torch.float64, device=DEVICE), scale - 127)[:, None, :]
     size = (full / scale).abs()
     down, up = torch.bucketize(size, between), torch.bucketize(size, between, right=True)
     found = numbers[torch.where(down % 2 == 0, down, up)] * torch.sign(full) * scale   # a tie: the even number
@@ -434,7 +434,7 @@ def exact(case, seed):
             codes = codes.long()
             if c[side] == "e2m1":
                 codes = torch.stack((codes % 16, codes // 16), dim=-1).flatten(1)
-            power = torch.tensor([2.0 ** (i - 127) for i in range(256)], dtype=torch.float64, device=DEVICE)[scales.long()]
+            power = torch.pow(torch.tensor(2.0, dtype=torch.float64, device=DEVICE), scales.double() - 127)
             sides.append((tables[c[side]][codes] * power.repeat_interleave(BLOCK, dim=1))[:, :c["inner"]])
         y = torch.matmul(sides[0], sides[1].t())
         return {"out": y + s["out"].double() if c["accumulate"] else y}
