@@ -29,6 +29,7 @@ HH_STATIC_SCRATCH_BYTES = 128 << 20
 HH_CLIP_WORKSPACE_BYTES = 8192
 HH_MX_NONE, HH_MX_E4M3, HH_MX_E2M1 = 0, 1, 2
 HH_MX_PAD = 256
+HH_MX_SUMS_F32, HH_MX_SUMS_FAST = 0, 1
 
 WEIGHT_FIELDS = ("g_attn", "wq", "wk", "wv", "wo", "g_mlp", "w_gate", "w_up", "w_down")
 EXPORTS = ("hh_last_error", "hh_ctx_create", "hh_ctx_destroy", "hh_ctx_reserve", "hh_layer_flops", "hh_layer_sizes",
@@ -127,7 +128,7 @@ class hh_add_norm_cfg(C.Structure):
 
 class hh_mx_product_cfg(C.Structure):
     _fields_ = [("m", C.c_int32), ("n", C.c_int32), ("k", C.c_int32), ("a_format", C.c_int32), ("b_format", C.c_int32), ("dtype", C.c_int32),
-                ("ldc", C.c_int64)]
+                ("ldc", C.c_int64), ("sums", C.c_int32)]
 
 
 class HHError(RuntimeError):
@@ -536,8 +537,8 @@ def hh_add_norm_bwd(ctx, cfg: hh_add_norm_cfg, drop: hh_dropout_cfg | None, h, g
                                int(accumulate), _ptr(workspace), stream))
 
 
-def make_mx_product_cfg(m, n, k, a_format, b_format, dtype=HH_BF16, ldc=None) -> hh_mx_product_cfg:
-    return hh_mx_product_cfg(m, n, k, a_format, b_format, dtype, n if ldc is None else ldc)
+def make_mx_product_cfg(m, n, k, a_format, b_format, dtype=HH_BF16, ldc=None, sums=HH_MX_SUMS_F32) -> hh_mx_product_cfg:
+    return hh_mx_product_cfg(m, n, k, a_format, b_format, dtype, n if ldc is None else ldc, sums)
 
 
 def hh_mx_product_sizes(cfg: hh_mx_product_cfg) -> int:

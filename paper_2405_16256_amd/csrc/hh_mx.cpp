@@ -179,13 +179,14 @@ extern "C" int hh_add_norm_bwd(hh_ctx* ctx, const hh_add_norm_cfg* cfg, const hh
 static int check_product(const hh_mx_product_cfg* c, MxProduct& p) {
     if (!c) return fail(HH_ERR_INVALID_ARG, "cfg is NULL");
     TRY(check_dtype(c->dtype)); TRY(check_format(c->a_format, "cfg.a_format")); TRY(check_format(c->b_format, "cfg.b_format"));
+    if (c->sums != HH_MX_SUMS_F32 && c->sums != HH_MX_SUMS_FAST) return fail(HH_ERR_INVALID_ARG, "cfg.sums %d is not HH_MX_SUMS_F32/HH_MX_SUMS_FAST", c->sums);
     if (c->m <= 0 || c->n <= 0 || c->k <= 0) return fail(HH_ERR_INVALID_ARG, "cfg has a non-positive dimension");
     TRY(check_ld(c->ldc, c->n, "cfg.ldc"));
     const int64_t width = mx_width(c->k), most = (1LL << 32) - (1LL << 25);
     if (c->m * width / (c->a_format == HH_MX_E4M3 ? 1 : 2) >= most || c->n * width / (c->b_format == HH_MX_E4M3 ? 1 : 2) >= most)
         return fail(HH_ERR_UNSUPPORTED_SHAPE, "an operand of %d or %d rows of %d values reaches 2^32 bytes", c->m, c->n, c->k);
     if ((int64_t)c->m * c->n > 1LL << 33) return fail(HH_ERR_UNSUPPORTED_SHAPE, "a result of %d x %d exceeds 2^33 elements", c->m, c->n);
-    p = MxProduct{c->m, c->n, c->k, c->a_format, c->b_format, {}, {}, nullptr, c->ldc, c->dtype == HH_F32, 0};
+    p = MxProduct{c->m, c->n, c->k, c->a_format, c->b_format, {}, {}, nullptr, c->ldc, c->dtype == HH_F32, 0, c->sums == HH_MX_SUMS_FAST};
     return HH_OK;
 }
 

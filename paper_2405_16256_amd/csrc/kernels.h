@@ -210,7 +210,8 @@ hipError_t add_norm_bwd(int dtype, const Drop& d, int rows, int hidden, float ep
 hipError_t mx_quantise(int dtype, long rows, long cols, const void* x, long ldx, int format, const MxRows& by_row, const MxRows& by_column,
                        hipStream_t st);
 hipError_t mx_values(int dtype, long rows, long k, int format, const MxRows& q, void* y, long ldy, hipStream_t st);
-struct MxProduct { int M, N, K; int fa, fb; MxRows a, b; void* C; long ldc; int f32, accumulate; };
+// fast: sums may be of fewer bits than fp32's
+struct MxProduct { int M, N, K; int fa, fb; MxRows a, b; void* C; long ldc; int f32, accumulate, fast; };
 size_t mx_product_workspace(const MxProduct& p);
 hipError_t mx_product(const MxProduct& p, void* ws, hipStream_t st);
 

@@ -15,8 +15,8 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // chip has its whole share under way at once: 1x4096x11008 E4M3 by E2M1 6.5 us (23 MB, 3.6 TB/s; a launch that does nothing is 2 of them),
 // E2M1 twice 5.9; 16 rows of 4096x4096 4.7 to 6.6.
 //
-// Of 16 rows x 128 k lane l holds row l % 16 and, with q = l / 16, of E2M1 the codes 32 q .. 32 q + 31, of E4M3 (and WIDE) 16 q .. 16 q + 15 and
-// 64 + 16 q .. 64 + 16 q + 15; its scale is that of k = 32 q .. 32 q + 31.
+// Of 16 rows x 128 k lane l holds row l % 16 and, with q = l / 16, the codes 32 q .. 32 q + 31 with their one scale: of E2M1 on both sides what the
+// matrix instruction takes, otherwise (WIDE) eight at a time, widened, whatever k they are of, the same for both operands.
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 // The conversions take a scale's exponent alone, of which 0 is 2^-127 and 255 NaN to them.
 __device__ __forceinline__ float scale_bits(uint32_t byte) { return __uint_as_float(byte << 23); }
@@ -32,50 +32,39 @@ template <> __device__ __forceinline__ bf16x8 widen8<MX_E2M1>(uint32_t lo, uint3
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-template <int F, bool WIDE>
+template <int F>
 struct RowUnit {   // 256 k of the lane's row
     i32x4 v[F == MX_E4M3 ? 4 : 2];
     uint2 s;
     __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int unit, int q) {
-        if constexpr (F == MX_E4M3) {
+        constexpr int HALF = F == MX_E4M3 ? 2 : 1;   // loads
 #pragma unroll
-            for (int i = 0; i < 4; i++) v[i] = *reinterpret_cast<const i32x4*>(codes + 256 * (long)unit + 64 * i + 16 * q);
-        } else if constexpr (WIDE) {
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const i32x2 a = *reinterpret_cast<const i32x2*>(codes + 128 * (long)unit + 64 * i + 8 * q);
-                const i32x2 b = *reinterpret_cast<const i32x2*>(codes + 128 * (long)unit + 64 * i + 32 + 8 * q);
-                v[i] = i32x4{a[0], a[1], b[0], b[1]};
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; i++) v[i] = *reinterpret_cast<const i32x4*>(codes + 128 * (long)unit + 64 * i + 16 * q);
-        }
+        for (int i = 0; i < 2 * HALF; i++)
+            v[i] = *reinterpret_cast<const i32x4*>(codes + (128 * (long)unit + 64 * (i / HALF) + 16 * q) * HALF + 16 * (i % HALF));
         s = *reinterpret_cast<const uint2*>(scales + 8 * (long)unit);
     }
-    __device__ __forceinline__ i32x8 operand(int half) const {
-        if constexpr (F == MX_E4M3) {
-            const i32x4 a = v[2 * half], b = v[2 * half + 1];
-            return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        } else {
-            const i32x4 a = v[half];
-            return i32x8{a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-        }
+    __device__ __forceinline__ i32x8 operand(int half) const {   // E2M1, as the matrix instruction takes it
+        const i32x4 a = v[half];
+        return i32x8{a[0], a[1], a[2], a[3], 0, 0, 0, 0};
     }
-    __device__ __forceinline__ int scale(int half, int q) const { return (int)((half ? s.y : s.x) >> (8 * q)); }
-    // 8 codes of the 16 at k = 128 half + 64 part + 16 q, widened
-    __device__ __forceinline__ bf16x8 widened(int half, int part, int eight, int q) const {
-        const float x = scale_bits((half ? s.y : s.x) >> (16 * part + 8 * (q >> 1)) & 255u);
-        if constexpr (F == MX_E4M3) return widen8<F>((uint32_t)v[2 * half + part][2 * eight], (uint32_t)v[2 * half + part][2 * eight + 1], x);
-        else return widen8<F>((uint32_t)v[half][2 * part + eight], 0u, x);
+    __device__ __forceinline__ uint32_t scale(int half, int q) const { return (half ? s.y : s.x) >> (8 * q); }
+    // codes 8 eight .. of the 32
+    __device__ __forceinline__ bf16x8 widened(int half, int eight, float scale) const {
+        if constexpr (F == MX_E4M3) {
+            const i32x4 a = v[2 * half + (eight >> 1)];
+            return widen8<F>((uint32_t)a[2 * (eight & 1)], (uint32_t)a[2 * (eight & 1) + 1], scale);
+        } else {
+            return widen8<F>((uint32_t)v[half][eight], 0u, scale);
+        }
     }
 };
 
 template <int F> constexpr int FORMAT = F == MX_E4M3 ? 0 : 4;   // of the matrix instruction
 struct MxRowsProblem { const uint8_t *a, *b, *sa, *sb; void* C; long ldc; int M, N, units, accumulate; uint32_t pitch_a, pitch_b, pitch_s; };
 
-template <int FA, int FB, bool WIDE, typename TC, int TM, int NW>
+template <int FA, int FB, typename TC, int TM, int NW>
 __global__ __launch_bounds__(64 * NW) void k_product_rows(MxRowsProblem p) {
+    constexpr bool WIDE = FA == MX_E4M3 || FB == MX_E4M3;
     __shared__ float part[NW][TM][256];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63, q = lane >> 4, l = lane & 15;
     const int n0 = (int)blockIdx.x * 16;
@@ -93,25 +82,29 @@ __global__ __launch_bounds__(64 * NW) void k_product_rows(MxRowsProblem p) {
     }
 #pragma unroll 4
     for (int u = wave; u < p.units; u += NW) {
-        RowUnit<FB, WIDE> ub;
-        RowUnit<FA, WIDE> ua[TM];
+        RowUnit<FB> ub;
+        RowUnit<FA> ua[TM];
         ub.load(b, sb, u, q);
 #pragma unroll
         for (int i = 0; i < TM; i++) ua[i].load(a[i], sa[i], u, q);
 #pragma unroll
         for (int half = 0; half < 2; half++) {
             if constexpr (WIDE) {
+                const float xb = scale_bits(ub.scale(half, q) & 255u);
+                float xa[TM];
 #pragma unroll
-                for (int x = 0; x < 4; x++) {
-                    const bf16x8 w = ub.widened(half, x >> 1, x & 1, q);
+                for (int i = 0; i < TM; i++) xa[i] = scale_bits(ua[i].scale(half, q) & 255u);
 #pragma unroll
-                    for (int i = 0; i < TM; i++) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, ua[i].widened(half, x >> 1, x & 1, q), acc[i], 0, 0, 0);
+                for (int eight = 0; eight < 4; eight++) {
+                    const bf16x8 w = ub.widened(half, eight, xb);
+#pragma unroll
+                    for (int i = 0; i < TM; i++) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, ua[i].widened(half, eight, xa[i]), acc[i], 0, 0, 0);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < TM; i++)
                     acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ub.operand(half), ua[i].operand(half), acc[i], FORMAT<FB>, FORMAT<FA>, 0,
-                                                                            ub.scale(half, q), 0, ua[i].scale(half, q));
+                                                                            (int)ub.scale(half, q), 0, (int)ua[i].scale(half, q));
             }
         }
     }
@@ -480,6 +473,10 @@ __global__ __launch_bounds__(256) void k_sum_shares(const float* __restrict__ pa
 // 4096x4096x4096 118, 87, 59.5.
 enum { ROWS_16, ROWS_32, TILES_64, TILES_128, TILES_256 };
 struct MxPlan { int kernel, split; };
+// The instruction for E4M3 adds its products in fewer bits than fp32's: taken only where the caller allows it, the result has fewer still and it is
+// faster, which it is not for few rows: 1, 16 and 32 x 4096 x 4096, E4M3 by E2M1, 4.8, 6.4 and 8.9 us widened, 5.1, 6.7 and 9.1 by that
+// instruction; E4M3 twice 6.4, 7.8, 10.6 and 6.4, 7.7, 10.1.
+static bool widened(const MxProduct& p) { return (p.fa == MX_E4M3 || p.fb == MX_E4M3) && (p.f32 || !p.fast || p.M <= 32); }
 constexpr int CUS = 256;
 static long tiles_of(const MxProduct& p, int b) { return (long)((p.M + b - 1) / b) * ((p.N + b - 1) / b); }
 static MxPlan plan(const MxProduct& p) {
@@ -488,7 +485,7 @@ static MxPlan plan(const MxProduct& p) {
     const bool four = p.fa == MX_E2M1 && p.fb == MX_E2M1;
     constexpr float STAGE_US[3][3] = {{0.32f, 0.78f, 2.15f}, {0.26f, 0.65f, 1.85f}, {0.46f, 1.05f, 3.4f}};   // E2M1, E4M3, widened
     constexpr float ENDS_US[3] = {0.7f, 2.2f, 3.5f};
-    const float* const us = STAGE_US[four ? 0 : p.f32 ? 2 : 1];
+    const float* const us = STAGE_US[four ? 0 : widened(p) ? 2 : 1];
     const int stages = (p.K + (four ? 255 : 127)) / (four ? 256 : 128);
     MxPlan best{TILES_64, 1};
     float least = 0.f;
@@ -533,21 +530,21 @@ static hipError_t launch_tiles(const MxProduct& q, int split, void* ws, hipStrea
     }
     return hipGetLastError();
 }
-template <int FA, int FB, bool WIDE, typename TC, int TM>
+template <int FA, int FB, typename TC, int TM>
 static hipError_t launch_rows(const MxProduct& q, hipStream_t st) {
     const long width = mx_width(q.K);
     const MxRowsProblem p{q.a.codes, q.b.codes, q.a.scales, q.b.scales, q.C, q.ldc, q.M, q.N, (int)(width / 256), q.accumulate,
                           (uint32_t)(FA == MX_E4M3 ? width : width / 2), (uint32_t)(FB == MX_E4M3 ? width : width / 2), (uint32_t)(width / MX_BLOCK)};
     const int grid = (q.N + 15) / 16;
-    if (p.units <= 4) k_product_rows<FA, FB, WIDE, TC, TM, 4><<<grid, 256, 0, st>>>(p);
-    else if (p.units <= 8) k_product_rows<FA, FB, WIDE, TC, TM, 8><<<grid, 512, 0, st>>>(p);
-    else k_product_rows<FA, FB, WIDE, TC, TM, 16><<<grid, 1024, 0, st>>>(p);
+    if (p.units <= 4) k_product_rows<FA, FB, TC, TM, 4><<<grid, 256, 0, st>>>(p);
+    else if (p.units <= 8) k_product_rows<FA, FB, TC, TM, 8><<<grid, 512, 0, st>>>(p);
+    else k_product_rows<FA, FB, TC, TM, 16><<<grid, 1024, 0, st>>>(p);
     return hipGetLastError();
 }
 
 // The kernel and the shares of k of a product, 100 kernel + shares: for tests, not in the public headers.
-extern "C" int hh_internal_mx_plan(int m, int n, int k, int a_format, int b_format, int f32) {
-    const MxPlan l = plan(MxProduct{m, n, k, a_format, b_format, {}, {}, nullptr, n, f32, 0});
+extern "C" int hh_internal_mx_plan(int m, int n, int k, int a_format, int b_format, int how) {
+    const MxPlan l = plan(MxProduct{m, n, k, a_format, b_format, {}, {}, nullptr, n, how == 1, 0, how == 2});
     return 100 * l.kernel + l.split;
 }
 
@@ -566,8 +563,8 @@ static hipError_t run_product(const MxProduct& p, void* ws, hipStream_t st) {
     constexpr int NS = FA == FB ? 2 : 3, KS = STAGE_K<FA, FB>;
     const MxPlan l = plan(p);
     switch (l.kernel) {
-        case ROWS_16: return launch_rows<FA, FB, WIDE, TC, 1>(p, st);
-        case ROWS_32: return launch_rows<FA, FB, WIDE, TC, 2>(p, st);
+        case ROWS_16: return launch_rows<FA, FB, TC, 1>(p, st);
+        case ROWS_32: return launch_rows<FA, FB, TC, 2>(p, st);
         case TILES_64: return launch_tiles<FA, FB, WIDE, TC, WIDE ? 256 : KS, 64, 64, 2, 2, WIDE ? 2 : 3>(p, l.split, ws, st);
         case TILES_128:
             if (NS == 3 || tiles_of(p, 128) * l.split <= CUS) return launch_tiles<FA, FB, WIDE, TC, KS, 128, 128, 2, 2, 3>(p, l.split, ws, st);
@@ -579,7 +576,8 @@ hipError_t mx_product(const MxProduct& p, void* ws, hipStream_t st) {
     auto run = [&](auto fa, auto fb) {
         constexpr int FA = decltype(fa)::value, FB = decltype(fb)::value;
         constexpr bool WIDE = FA == MX_E4M3 || FB == MX_E4M3;
-        return p.f32 ? run_product<FA, FB, WIDE, float>(p, ws, st) : run_product<FA, FB, false, bf16_t>(p, ws, st);
+        if (p.f32) return run_product<FA, FB, WIDE, float>(p, ws, st);
+        return widened(p) ? run_product<FA, FB, WIDE, bf16_t>(p, ws, st) : run_product<FA, FB, false, bf16_t>(p, ws, st);
     };
     std::integral_constant<int, MX_E4M3> e8;
     std::integral_constant<int, MX_E2M1> e4;

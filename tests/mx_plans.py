@@ -1,0 +1,64 @@
+"""Which kernel a microscaled product takes, asked of the library without a GPU, sizes that reach each of them, and packed operands made on the
+GPU for them."""
+import torch
+
+from paper_2405_16256_amd import binding as hh
+from paper_2405_16256_amd import glue as L
+
+E4M3, E2M1 = hh.HH_MX_E4M3, hh.HH_MX_E2M1
+PAIRS = [(a, b) for a in (E4M3, E2M1) for b in (E4M3, E2M1)]
+BF16, F32, BF16_FAST = range(3)        # result and sums
+ROWS_16, ROWS_32, TILES_64, TILES_128, TILES_256 = range(5)
+# a size for each kernel of the product, whatever the formats
+SIZES = {ROWS_16: (7, 35, 1000), ROWS_32: (23, 70, 1100), TILES_64: (70, 130, 513), TILES_128: (2697, 715, 48), TILES_256: (516, 13083, 36)}
+
+
+def plan(m, n, k, fa, fb, how):
+    """-> (kernel, shares of k)"""
+    v = hh.lib.hh_internal_mx_plan(m, n, k, fa, fb, how)
+    return v // 100, v % 100
+
+
+def cfg(m, n, k, fa, fb, how, ldc=None):
+    return hh.make_mx_product_cfg(m, n, k, fa, fb, hh.HH_F32 if how == F32 else hh.HH_BF16, ldc, hh.HH_MX_SUMS_FAST if how == BF16_FAST else hh.HH_MX_SUMS_F32)
+
+
+def table(fmt):
+    """The numbers of a format by their code, NaN where a code is none."""
+    if fmt == E2M1:
+        half = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64)
+    else:
+        half = torch.tensor([m / 8 * 2.0 ** -6 for m in range(8)] + [(1 + m / 8) * 2.0 ** (e - 7) for e in range(1, 16) for m in range(8)], dtype=torch.float64)
+        half[127] = float("nan")
+    return torch.cat((half, -half)).to(L.DEV)
+
+
+class Operand:
+    """A packed tensor of codes [rows, k] (one a byte) and scales [rows, blocks of 32], with its values in fp64."""
+
+    def __init__(self, codes, scales, fmt):
+        rows, k = codes.shape
+        width = -(-k // 256) * 256
+        full = torch.zeros(rows, width, dtype=torch.uint8, device=L.DEV)
+        full[:, :k] = codes
+        self.scales = torch.zeros(rows, width // 32, dtype=torch.uint8, device=L.DEV)
+        self.scales[:, :scales.shape[1]] = scales
+        power = torch.tensor([2.0 ** (i - 127) for i in range(255)] + [float("nan")], dtype=torch.float64, device=L.DEV)
+        self.values = (table(fmt)[full.long()] * power[self.scales.long()].repeat_interleave(32, dim=1))[:, :k]
+        self.codes = (full[:, 0::2] | (full[:, 1::2] << 4)).contiguous() if fmt == E2M1 else full
+        self.struct = hh.make_mx(self.codes, self.scales)
+
+
+def product(ctx, a, b, m, n, k, fa, fb, how, old=None, extra=0):
+    """a b^T (+ old) [m, n] as the library forms it, in fp64; `extra` columns and two rows behind it stay as they are, and so does what lies
+    behind the workspace."""
+    f32 = how == F32
+    c = torch.full((m + 2, n + extra), 7.0, dtype=torch.float32 if f32 else torch.bfloat16, device=L.DEV)
+    if old is not None:
+        c[:m, :n] = old
+    p = cfg(m, n, k, fa, fb, how, n + extra)
+    ws = torch.full((hh.hh_mx_product_sizes(p) + 256,), 0xA5, dtype=torch.uint8, device=L.DEV)
+    hh.hh_mx_product(ctx, p, a.struct, b.struct, c, old is not None, ws, L.stream_ptr())
+    torch.cuda.synchronize()
+    assert bool((c[m:] == 7.0).all()) and bool((c[:, n:] == 7.0).all()) and bool((ws[-256:] == 0xA5).all())
+    return c[:m, :n].double()

@@ -1,0 +1,100 @@
+"""In how many bits a microscaled product is summed (include/hh_mx.h, hh_mx_sums).
+
+Into bfloat16 the sum's own error is under the result's rounding.  So the result is added to a C that holds its negative, rounded: what is left is small, and
+the rounding of that is smaller than the errors that are looked for."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2405_16256_amd import binding as hh
+from paper_2405_16256_amd import glue as L
+from tests.mx_plans import BF16, BF16_FAST, E2M1, E4M3, F32, PAIRS, SIZES, Operand, plan, product
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = hh.hh_ctx_create(0)
+    yield c
+    torch.cuda.synchronize()
+    hh.hh_ctx_destroy(c)
+
+
+def one_large_product(gen, rows, k, at, fmt, other):
+    """Rows of a format's largest number at `at` and +-1 small number everywhere else in the first 200 of k, at a scale of 1.  Small is so that
+    products of two are 2^-6 (E4M3 twice: next to 448 * 448 < 2^18), 2^-10 (E4M3 and E2M1: next to 2688 < 2^12) or 2^-2 (E2M1 twice: next to 36):
+    their sum with the large one, and every part of it, are numbers of fp32."""
+    most = {E4M3: 0x7E, E2M1: 0x07}[fmt]
+    small = {(E4M3, E4M3): 0x20, (E4M3, E2M1): 0x01, (E2M1, E4M3): 0x01, (E2M1, E2M1): 0x01}[fmt, other]   # 2^-3, 2^-9, 2^-1, 2^-1
+    sign = {E4M3: 0x80, E2M1: 0x08}[fmt]
+    codes = torch.zeros(rows, k, dtype=torch.uint8, device=L.DEV)
+    there = min(k, 200)
+    codes[:, :there] = small + sign * torch.randint(0, 2, (rows, there), device=L.DEV, generator=gen)
+    codes[:, at] = most
+    return Operand(codes, torch.full((rows, (k + 31) // 32), 127, device=L.DEV), fmt)
+
+
+@pytest.mark.parametrize("fa,fb", PAIRS)
+@pytest.mark.parametrize("kernel", sorted(SIZES))
+@pytest.mark.parametrize("how", (BF16, F32))
+def test_small_products_next_to_a_large_one_count(ctx, how, kernel, fa, fb):
+    """With the large product taken off, the sum of the small ones is left: at most 199 of one size, a number of bfloat16 too."""
+    m, n, k = SIZES[kernel]
+    assert plan(m, n, k, fa, fb, how) == (kernel, 1)
+    gen = torch.Generator(device=L.DEV).manual_seed(m + n + k)
+    large = {(E4M3, E4M3): 448.0 * 448, (E2M1, E2M1): 36.0}.get((fa, fb), 448.0 * 6)
+    for at in (0, k // 2, min(k, 200) - 1):
+        a, b = one_large_product(gen, m, k, at % min(k, 200), fa, fb), one_large_product(gen, n, k, at % min(k, 200), fb, fa)
+        want = a.values @ b.values.T - large
+        got = product(ctx, a, b, m, n, k, fa, fb, how, old=torch.full((m, n), -large, device=L.DEV))
+        assert torch.equal(got, want), (at, int((got != want).sum()), got.flatten()[:4].tolist(), want.flatten()[:4].tolist())
+
+
+def packed(ctx, gen, rows, k, fmt, outliers):
+    """Normal values packed by the library, and a 64th of them `outliers` times as large."""
+    x = torch.randn(rows, k, device=L.DEV, generator=gen)
+    if outliers:
+        x = torch.where(torch.rand(rows, k, device=L.DEV, generator=gen) < 1 / 64, x * outliers, x)
+    q = Operand(torch.zeros(rows, k, dtype=torch.uint8, device=L.DEV), torch.zeros(rows, 1, device=L.DEV), fmt)
+    hh.hh_mx_quantise(ctx, rows, k, hh.HH_F32, x, k, fmt, q.struct, None, L.stream_ptr())
+    q.values = torch.empty(rows, k, device=L.DEV)
+    hh.hh_mx_values(ctx, rows, k, fmt, q.struct, hh.HH_F32, q.values, k, L.stream_ptr())
+    q.values = q.values.double()
+    return q
+
+
+@pytest.mark.parametrize("fa,fb", PAIRS)
+@pytest.mark.parametrize("outliers", (0, 30, 100))
+@pytest.mark.parametrize("m", (9, 300))
+@pytest.mark.parametrize("how", (BF16, BF16_FAST))
+def test_error_of_a_sum(ctx, how, m, outliers, fa, fb):
+    """Of the size of the results, in the root of the mean square.  What is left after the rounded result is taken off is at most 2^-8 of it, evenly
+    spread, 2^-8 / sqrt(3), and so much of that is its own rounding's: 2^-16 / 3 of the result.  Then the sum's: of fp32, k roundings of either sign;
+    fast, with an E4M3 operand and more than 32 rows, what the header says."""
+    n, k = 260, 520
+    gen = torch.Generator(device=L.DEV).manual_seed(m + outliers)
+    a, b = packed(ctx, gen, m, k, fa, outliers), packed(ctx, gen, n, k, fb, outliers)
+    want = a.values @ b.values.T
+    old = -want.bfloat16()
+    got = product(ctx, a, b, m, n, k, fa, fb, how, old=old)
+    error = float((got - (want + old.double())).norm() / want.norm())
+    fast = how == BF16_FAST and m > 32 and E4M3 in (fa, fb)
+    bound = (1e-4 if outliers else 1.5e-5) if fast else np.sqrt(k) * E
+    print("error", fa, fb, how, m, outliers, "%.2e of %.2e" % (error, bound + 2.0 ** -16 / 3))
+    assert error <= bound + 2.0 ** -16 / 3
+
+
+@pytest.mark.parametrize("fa,fb", PAIRS)
+def test_fast_sums_of_few_rows_and_into_fp32_are_of_fp32(ctx, fa, fb):
+    gen = torch.Generator(device=L.DEV).manual_seed(5)
+    a, b = packed(ctx, gen, 33, 300, fa, 30), packed(ctx, gen, 70, 300, fb, 30)
+    for m in (1, 16, 32):
+        assert torch.equal(product(ctx, a, b, m, 70, 300, fa, fb, BF16), product(ctx, a, b, m, 70, 300, fa, fb, BF16_FAST))
+    c = [torch.empty(33, 70, device=L.DEV) for _ in range(2)]
+    for sums, out in zip((hh.HH_MX_SUMS_F32, hh.HH_MX_SUMS_FAST), c):
+        p = hh.make_mx_product_cfg(33, 70, 300, fa, fb, hh.HH_F32, sums=sums)
+        ws = torch.empty(hh.hh_mx_product_sizes(p), dtype=torch.uint8, device=L.DEV)
+        hh.hh_mx_product(ctx, p, a.struct, b.struct, out, 0, ws, L.stream_ptr())
+    assert torch.equal(*c)

@@ -1,0 +1,32 @@
+"""Plans of the microscaled product, and its refusals of sums that are not named.  Runs without a GPU."""
+import pytest
+
+from paper_2405_16256_amd import binding as hh
+from tests.mx_plans import BF16, BF16_FAST, E2M1, E4M3, F32, PAIRS, SIZES, plan
+
+
+def test_sums_that_are_not_named_are_refused():
+    q, a = hh.make_mx(1 << 20, 1 << 20), 1 << 20
+    for sums in (-1, 2):
+        cfg = hh.make_mx_product_cfg(4, 40, 100, E4M3, E2M1, sums=sums)
+        for call in (lambda: hh.hh_mx_product_sizes(cfg), lambda: hh.hh_mx_product(None, cfg, q, q, a, 0, a)):
+            with pytest.raises(hh.HHError) as e:
+                call()
+            assert e.value.code == hh.HH_ERR_INVALID_ARG and "sums" in str(e.value)
+
+
+def test_a_size_for_each_kernel():
+    for kernel, s in SIZES.items():
+        for fa, fb in PAIRS:
+            for how in (BF16, F32, BF16_FAST):
+                assert plan(*s, fa, fb, how)[0] == kernel, (s, fa, fb, how)
+
+
+def test_fast_sums_change_plans_of_tiles_with_an_e4m3_operand_alone():
+    """Elsewhere a call with fast sums is the call without."""
+    for m in (1, 16, 32, 33, 2000, 4096):
+        for fa, fb in PAIRS:
+            plans = [plan(m, 4096, 4096, fa, fb, how) for how in (BF16, BF16_FAST)]
+            if m <= 32 or (fa, fb) == (E2M1, E2M1):
+                assert plans[0] == plans[1]
+    assert plan(2000, 2600, 8192, E4M3, E4M3, BF16) == plan(2000, 2600, 8192, E4M3, E4M3, F32)
