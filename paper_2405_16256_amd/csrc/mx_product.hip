@@ -567,8 +567,9 @@ static hipError_t run_product(const MxProduct& p, void* ws, hipStream_t st) {
         case ROWS_32: return launch_rows<FA, FB, TC, 2>(p, st);
         case TILES_64: return launch_tiles<FA, FB, WIDE, TC, WIDE ? 256 : KS, 64, 64, 2, 2, WIDE ? 2 : 3>(p, l.split, ws, st);
         case TILES_128:
-            if (NS == 3 || tiles_of(p, 128) * l.split <= CUS) return launch_tiles<FA, FB, WIDE, TC, KS, 128, 128, 2, 2, 3>(p, l.split, ws, st);
-            return launch_tiles<FA, FB, WIDE, TC, KS, 128, 128, 2, 2, 2>(p, l.split, ws, st);
+            if constexpr (NS == 2)
+                if (tiles_of(p, 128) * l.split > CUS) return launch_tiles<FA, FB, WIDE, TC, KS, 128, 128, 2, 2, 2>(p, l.split, ws, st);
+            return launch_tiles<FA, FB, WIDE, TC, KS, 128, 128, 2, 2, 3>(p, l.split, ws, st);
         default: return launch_tiles<FA, FB, WIDE, TC, KS, 256, 256, 2, 4, NS>(p, l.split, ws, st);
     }
 }

@@ -1,4 +1,6 @@
 """Plans of the microscaled product, and its refusals of sums that are not named.  Runs without a GPU."""
+import re
+
 import pytest
 
 from paper_2405_16256_amd import binding as hh
@@ -30,3 +32,17 @@ def test_fast_sums_change_plans_of_tiles_with_an_e4m3_operand_alone():
             if m <= 32 or (fa, fb) == (E2M1, E2M1):
                 assert plans[0] == plans[1]
     assert plan(2000, 2600, 8192, E4M3, E4M3, BF16) == plan(2000, 2600, 8192, E4M3, E4M3, F32)
+
+
+def test_tiles_of_128_are_built_in_the_forms_that_are_launched():
+    """Of mixed formats with three stages alone; of two that are alike with two stages and with three."""
+    from paper_2405_16256_amd import build
+    from tests.test_kernel_resources import code_objects, kernels
+    with open(build.LIB, "rb") as f:
+        names = [k[".name"] for elf in code_objects(f.read()) for k in kernels(elf)]
+    stages = {}
+    for n in names:
+        m = re.search(r"k_product_tilesILi(\d)ELi(\d)ELb(\d)E([ft])Li(\d+)ELi128ELi128ELi2ELi2ELi(\d)E", n)
+        if m:
+            stages.setdefault((int(m[1]), int(m[2])), set()).add(int(m[6]))
+    assert stages == {p: {2, 3} if p[0] == p[1] else {3} for p in PAIRS}
