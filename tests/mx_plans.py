@@ -12,6 +12,9 @@ ROWS_16, ROWS_32, TILES_64, TILES_128, TILES_256 = range(5)
 # a size for each kernel of the product, whatever the formats
 SIZES = {ROWS_16: (7, 35, 1000), ROWS_32: (23, 70, 1100), TILES_64: (70, 130, 513), TILES_128: (2697, 715, 48), TILES_256: (516, 13083, 36)}
 
+# with shares of k: each number of them that tiles of 64 take, and tiles of 128 and 256; rows and columns that are odd
+SHARES = {TILES_64: [(513, 497, 2189), (45, 85, 2730), (35, 35, 1738), (33, 65, 8010)], TILES_128: [(851, 1179, 9505)], TILES_256: [(2131, 1967, 14112)]}
+
 
 def plan(m, n, k, fa, fb, how):
     """-> (kernel, shares of k)"""
@@ -62,3 +65,37 @@ def product(ctx, a, b, m, n, k, fa, fb, how, old=None, extra=0):
     torch.cuda.synchronize()
     assert bool((c[m:] == 7.0).all()) and bool((c[:, n:] == 7.0).all()) and bool((ws[-256:] == 0xA5).all())
     return c[:m, :n].double()
+
+
+def drawn(gen, rows, k, fmt):
+    """A packed tensor of any numbers of the format under scales of 2^-3 .. 2^3."""
+    codes = torch.randint(0, 256 if fmt == E4M3 else 16, (rows, k), dtype=torch.uint8, device=L.DEV, generator=gen)
+    if fmt == E4M3:
+        codes[codes % 128 == 127] = 0
+    return Operand(codes, torch.randint(124, 131, (rows, (k + 31) // 32), dtype=torch.uint8, device=L.DEV, generator=gen), fmt)
+
+
+def check(ctx, m, n, k, fa, fb, how, accumulate=False, extra=0, seed=0):
+    """One product of drawn operands against fp64.  The sum: k products, each added with an error of at most 2^-23 of the sum of magnitudes so
+    far; fast with an E4M3 operand and more than 32 rows, each of the 64 products of an instruction cut at 2^-16 of the largest of them, 2^-10
+    of the sum of their magnitudes.  Then half a step of the result's type, and one of fp32 where the old value is added."""
+    gen = torch.Generator(device=L.DEV).manual_seed(seed + m + 3 * n + 5 * k)
+    a, b = drawn(gen, m, k, fa), drawn(gen, n, k, fb)
+    want, size = a.values @ b.values.T, a.values.abs() @ b.values.T.abs()
+    old = None
+    if accumulate:   # as large as the sums are
+        old = torch.randn(m, n, device=L.DEV, generator=gen) * float(want.std())
+        old = old if how == F32 else old.bfloat16()
+        want += old.double()
+    got = product(ctx, a, b, m, n, k, fa, fb, how, old, extra)
+    fast = how == BF16_FAST and m > 32 and E4M3 in (fa, fb)
+    half = 2.0 ** -24 if how == F32 else 2.0 ** -8
+    bound = (2.0 ** -10 if fast else 2.0 ** -23 * k) * size + half * want.abs()
+    if accumulate:
+        bound += 2.0 ** -23 * (old.double().abs() + want.abs())
+    bad = (got - want).abs() > bound
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist())
+    # roundings of either sign grow with the root of their number; the result's own, evenly spread, is half a step over the root of three
+    sums = 2.0 ** -12 if fast else 2.0 ** -22 * k ** 0.5
+    error = float((got - want).norm() / want.norm())
+    assert error <= sums + half / 3 ** 0.5, (error, sums)

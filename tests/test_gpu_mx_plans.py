@@ -1,0 +1,24 @@
+"""Every kernel of the microscaled product, in every form that a plan gives it, for each pair of formats, result and sums."""
+import pytest
+import torch
+
+from paper_2405_16256_amd import binding as hh
+from tests.mx_plans import BF16, BF16_FAST, F32, PAIRS, SHARES, check
+
+pytestmark = pytest.mark.gpu
+HOWS = (BF16, F32, BF16_FAST)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = hh.hh_ctx_create(0)
+    yield c
+    torch.cuda.synchronize()
+    hh.hh_ctx_destroy(c)
+
+
+@pytest.mark.parametrize("fa,fb", PAIRS)
+@pytest.mark.parametrize("how", HOWS)
+@pytest.mark.parametrize("m,n,k", [s for sizes in SHARES.values() for s in sizes])
+def test_shares_of_k(ctx, m, n, k, how, fa, fb):
+    check(ctx, m, n, k, fa, fb, how, extra=3)

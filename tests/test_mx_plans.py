@@ -4,7 +4,7 @@ import re
 import pytest
 
 from paper_2405_16256_amd import binding as hh
-from tests.mx_plans import BF16, BF16_FAST, E2M1, E4M3, F32, PAIRS, SIZES, plan
+from tests.mx_plans import BF16, BF16_FAST, E2M1, E4M3, F32, PAIRS, SHARES, SIZES, plan
 
 
 def test_sums_that_are_not_named_are_refused():
@@ -22,6 +22,15 @@ def test_a_size_for_each_kernel():
         for fa, fb in PAIRS:
             for how in (BF16, F32, BF16_FAST):
                 assert plan(*s, fa, fb, how)[0] == kernel, (s, fa, fb, how)
+
+
+def test_sizes_in_shares_of_k():
+    """Tiles of each size, for each pair of formats, result and sums."""
+    for fa, fb in PAIRS:
+        for how in (BF16, F32, BF16_FAST):
+            for kernel, sizes in SHARES.items():
+                plans = [plan(*s, fa, fb, how) for s in sizes]
+                assert {p[0] for p in plans} == {kernel} and max(p[1] for p in plans) > 1, (kernel, plans, fa, fb, how)
 
 
 def test_fast_sums_change_plans_of_tiles_with_an_e4m3_operand_alone():
