@@ -15,6 +15,9 @@ SIZES = {ROWS_16: (7, 35, 1000), ROWS_32: (23, 70, 1100), TILES_64: (70, 130, 51
 # with shares of k: each number of them that tiles of 64 take, and tiles of 128 and 256; rows and columns that are odd
 SHARES = {TILES_64: [(513, 497, 2189), (45, 85, 2730), (35, 35, 1738), (33, 65, 8010)], TILES_128: [(851, 1179, 9505)], TILES_256: [(2131, 1967, 14112)]}
 
+# tiles of 128, more of them than compute units: another number of stages where the formats are alike
+MANY_128 = (2409, 2124, 261)
+
 
 def plan(m, n, k, fa, fb, how):
     """-> (kernel, shares of k)"""

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2405_16256_amd import binding as hh
-from tests.mx_plans import BF16, BF16_FAST, F32, PAIRS, SHARES, check
+from tests.mx_plans import BF16, BF16_FAST, F32, MANY_128, PAIRS, SHARES, SIZES, check
 
 pytestmark = pytest.mark.gpu
 HOWS = (BF16, F32, BF16_FAST)
@@ -22,3 +22,10 @@ def ctx():
 @pytest.mark.parametrize("m,n,k", [s for sizes in SHARES.values() for s in sizes])
 def test_shares_of_k(ctx, m, n, k, how, fa, fb):
     check(ctx, m, n, k, fa, fb, how, extra=3)
+
+
+@pytest.mark.parametrize("fa,fb", PAIRS)
+@pytest.mark.parametrize("how", HOWS)
+@pytest.mark.parametrize("m,n,k", [*SIZES.values(), MANY_128, *(s for sizes in SHARES.values() for s in sizes)])
+def test_what_is_there_is_added_to(ctx, m, n, k, how, fa, fb):
+    check(ctx, m, n, k, fa, fb, how, accumulate=True, extra=n % 4 + 1)

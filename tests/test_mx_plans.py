@@ -4,7 +4,7 @@ import re
 import pytest
 
 from paper_2405_16256_amd import binding as hh
-from tests.mx_plans import BF16, BF16_FAST, E2M1, E4M3, F32, PAIRS, SHARES, SIZES, plan
+from tests.mx_plans import BF16, BF16_FAST, E2M1, E4M3, F32, MANY_128, PAIRS, SHARES, SIZES, TILES_128, plan
 
 
 def test_sums_that_are_not_named_are_refused():
@@ -31,6 +31,14 @@ def test_sizes_in_shares_of_k():
             for kernel, sizes in SHARES.items():
                 plans = [plan(*s, fa, fb, how) for s in sizes]
                 assert {p[0] for p in plans} == {kernel} and max(p[1] for p in plans) > 1, (kernel, plans, fa, fb, how)
+
+
+def test_a_size_of_more_tiles_of_128_than_compute_units():
+    m, n, _ = MANY_128
+    assert -(-m // 128) * -(-n // 128) > 256
+    for fa, fb in PAIRS:
+        for how in (BF16, F32, BF16_FAST):
+            assert plan(*MANY_128, fa, fb, how) == (TILES_128, 1), (fa, fb, how)
 
 
 def test_fast_sums_change_plans_of_tiles_with_an_e4m3_operand_alone():
