@@ -18,6 +18,9 @@ SHARES = {TILES_64: [(513, 497, 2189), (45, 85, 2730), (35, 35, 1738), (33, 65, 
 # tiles of 128, more of them than compute units: another number of stages where the formats are alike
 MANY_128 = (2409, 2124, 261)
 
+# few rows, four, eight and sixteen waves, each with one unit of 256 k and with several; no row or column more than there is room for, and all
+FEW = [(m, n, k) for m in (1, 7, 16, 17, 23, 31, 32) for n, k in ((33, 31), (19, 1000), (70, 1100), (48, 2048), (65, 2300), (35, 9001))]
+
 
 def plan(m, n, k, fa, fb, how):
     """-> (kernel, shares of k)"""
@@ -98,7 +101,9 @@ def check(ctx, m, n, k, fa, fb, how, accumulate=False, extra=0, seed=0):
         bound += 2.0 ** -23 * (old.double().abs() + want.abs())
     bad = (got - want).abs() > bound
     assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist())
-    # roundings of either sign grow with the root of their number; the result's own, evenly spread, is half a step over the root of three
+    # Roundings of either sign grow with the root of their number.  The result's own: each at most half a step of its value, so half in the norm too;
+    # evenly spread, with results that begin at any place between two powers of two, half (0.54 / 3)^0.5 = 0.43 in the mean.  Over 100 results
+    # (of 2^14, which are weighed by their size) the root of the mean square is off by a twentieth of that: 0.58 is seven such deviations off.
     sums = 2.0 ** -12 if fast else 2.0 ** -22 * k ** 0.5
     error = float((got - want).norm() / want.norm())
-    assert error <= sums + half / 3 ** 0.5, (error, sums)
+    assert error <= sums + half * (0.58 if m * n >= 1 << 14 else 1.0), (error, sums)

@@ -4,7 +4,7 @@ import re
 import pytest
 
 from paper_2405_16256_amd import binding as hh
-from tests.mx_plans import BF16, BF16_FAST, E2M1, E4M3, F32, MANY_128, PAIRS, SHARES, SIZES, TILES_128, plan
+from tests.mx_plans import BF16, BF16_FAST, E2M1, E4M3, F32, FEW, MANY_128, PAIRS, ROWS_16, ROWS_32, SHARES, SIZES, TILES_128, plan
 
 
 def test_sums_that_are_not_named_are_refused():
@@ -39,6 +39,18 @@ def test_a_size_of_more_tiles_of_128_than_compute_units():
     for fa, fb in PAIRS:
         for how in (BF16, F32, BF16_FAST):
             assert plan(*MANY_128, fa, fb, how) == (TILES_128, 1), (fa, fb, how)
+
+
+def test_sizes_of_few_rows():
+    """Both kernels with every number of waves (up to 4 units of 256 k: 4, up to 8: 8, more: 16), a wave with one unit and with several."""
+    seen = set()
+    for m, n, k in FEW:
+        kernel, _ = plan(m, n, k, E4M3, E2M1, BF16)
+        units = -(-k // 256)
+        waves = 4 if units <= 4 else 8 if units <= 8 else 16
+        assert kernel == (ROWS_16 if m <= 16 else ROWS_32)
+        seen.add((kernel, waves, units > waves))
+    assert seen == {(kernel, waves, False) for kernel in (ROWS_16, ROWS_32) for waves in (4, 8, 16)} | {(kernel, 16, True) for kernel in (ROWS_16, ROWS_32)}
 
 
 def test_fast_sums_change_plans_of_tiles_with_an_e4m3_operand_alone():
