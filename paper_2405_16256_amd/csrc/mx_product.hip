@@ -18,9 +18,10 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // Of 16 rows x 128 k lane l holds row l % 16 and, with q = l / 16, the codes 32 q .. 32 q + 31 with their one scale: of E2M1 on both sides what the
 // matrix instruction takes, otherwise (WIDE) eight at a time, widened, whatever k they are of, the same for both operands.
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
-// The conversions take a scale's exponent alone, of which 0 is 2^-127 and 255 NaN to them.
+// The conversions take a scale's exponent alone, of which 0 is 2^-127 and 255 NaN to them.  What they make is exact where bfloat16 holds
+// it, rounded to nearest below 2^-130 and infinite from 2^128 on.
 __device__ __forceinline__ float scale_bits(uint32_t byte) { return __uint_as_float(byte << 23); }
-template <int F> __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale);   // 8 codes (E2M1: of lo) with their scale, exactly
+template <int F> __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale);   // 8 codes (E2M1: of lo) with their scale
 template <> __device__ __forceinline__ bf16x8 widen8<MX_E4M3>(uint32_t lo, uint32_t hi, float scale) {
     const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
     const bf16x2v c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);

@@ -98,3 +98,30 @@ def test_fast_sums_of_few_rows_and_into_fp32_are_of_fp32(ctx, fa, fb):
         ws = torch.empty(hh.hh_mx_product_sizes(p), dtype=torch.uint8, device=L.DEV)
         hh.hh_mx_product(ctx, p, a.struct, b.struct, out, 0, ws, L.stream_ptr())
     assert torch.equal(*c)
+
+
+@pytest.mark.parametrize("fmt", (E4M3, E2M1))
+@pytest.mark.parametrize("rows", (127, 20))
+@pytest.mark.parametrize("how", (BF16, F32))
+def test_values_outside_of_bfloat16(ctx, how, rows, fmt):
+    """Every number of a format under the scales at their ends, times a power of two on the other side (E4M3, so that both sides are widened): exact
+    where bfloat16 holds the value, otherwise that of the value rounded to it, infinity above."""
+    n = 70
+    numbers = torch.arange(rows, device=L.DEV) + (127 - rows if fmt == E4M3 else 0)
+    codes = torch.zeros(rows, 300, dtype=torch.uint8, device=L.DEV)
+    codes[:, 131] = numbers % (127 if fmt == E4M3 else 8)
+    for scale in (0, 1, 2, 3, 4, 100, 245, 246, 247, 250, 252, 253, 254):
+        a = Operand(codes, torch.full((rows, 10), scale, device=L.DEV), fmt)
+        one = torch.zeros(n, 300, dtype=torch.uint8, device=L.DEV)
+        one[:, 131] = 0x38
+        b = Operand(one, torch.full((n, 10), 227 if scale < 100 else 27 if scale > 100 else 127, device=L.DEV), E4M3)
+        want = a.values[:, 131:132].bfloat16().double() * b.values[:, 131:132].T
+        if (3 if fmt == E4M3 else 0) <= scale <= (246 if fmt == E4M3 else 252):
+            assert torch.equal(want, a.values[:, 131:132] * b.values[:, 131:132].T)
+        for x, y, m, k in ((a, b, rows, n), (b, a, n, rows)):
+            got = product(ctx, x, y, m, k, 300, fmt if x is a else E4M3, E4M3 if x is a else fmt, how)
+            assert torch.equal(got, want if x is a else want.T), (scale, got[:, 0].tolist(), want[:, 0].tolist())
+        for t, code in ((torch.bfloat16, hh.HH_BF16), (torch.float32, hh.HH_F32)):
+            v = torch.empty(rows, 300, dtype=t, device=L.DEV)
+            hh.hh_mx_values(ctx, rows, 300, fmt, a.struct, code, v, 300, L.stream_ptr())
+            assert torch.equal(v.double(), a.values.to(t).double()), scale
