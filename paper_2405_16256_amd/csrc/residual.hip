@@ -244,7 +244,7 @@ __global__ __launch_bounds__(row_threads<W>(), (RAGGED ? 2 : grad_waves<T, CH>()
             }
         }
         row_sums<W>(ss, dot, red[turn]);
-        const float r = inverse_root(ss, hidden, eps), k = r * r * (dot / (float)hidden);
+        const float r = inverse_root(ss, hidden, eps), k = r * (r * (dot / (float)hidden));   // r^2 may be past fp32
 #pragma unroll
         for (int c = 0; c < CH; c++) {
             __builtin_amdgcn_sched_barrier(0);   // a chunk at a time
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(1024) void k_add_norm_bwd_wide(Drop d, int rows, in
             }
         }
         row_sums<16>(ss, dot, red[turn]);
-        const float r = inverse_root(ss, hidden, eps), k = r * r * (dot / (float)hidden);
+        const float r = inverse_root(ss, hidden, eps), k = r * (r * (dot / (float)hidden));   // r^2 may be past fp32
         for (int c = (int)threadIdx.x; c < chunks; c += 1024) {
             const int at = 8 * c, n = hidden - at;
             Eight<T> e, rd{};

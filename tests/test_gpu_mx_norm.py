@@ -1,0 +1,49 @@
+"""Gradients of hh_add_norm_bwd (hh_mx.h) where fp32 is short of exponents or of bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx_oracle as O
+from paper_2405_16256_amd import binding as hh
+from paper_2405_16256_amd import glue as L
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+TYPES = {"bf16": (torch.bfloat16, hh.HH_BF16), "f32": (torch.float32, hh.HH_F32)}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = hh.hh_ctx_create(0)
+    yield c
+    torch.cuda.synchronize()
+    hh.hh_ctx_destroy(c)
+
+
+def gradients(ctx, h, g, dxn, eps, dtype):
+    """-> dx, dg of the library, fp64"""
+    dt, code = TYPES[dtype]
+    rows, hidden = h.shape
+    cfg = hh.make_add_norm_cfg(rows, hidden, eps, code)
+    h, g, dxn = (torch.from_numpy(np.ascontiguousarray(t)).to(L.DEV, dt) for t in (h, g, dxn))
+    dx, dg = torch.empty_like(h), torch.empty(hidden, device=L.DEV)
+    ws = torch.empty(hh.hh_add_norm_sizes(cfg), dtype=torch.uint8, device=L.DEV)
+    hh.hh_add_norm_bwd(ctx, cfg, None, h, g, dxn, None, dx, None, dg, 0, ws, L.stream_ptr())
+    return dx.cpu().double().numpy(), dg.cpu().double().numpy()
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("hidden", (64, 1024, 4096, 32768))
+@pytest.mark.parametrize("power", (-70, -66, 0, 50))
+def test_rows_whose_inverse_root_has_no_square(ctx, dtype, hidden, power):
+    """Rows of +-2^power without eps: r = 2^-power, of which fp32 does not hold the square below 2^-64.  Tolerances of the other gradients' tests:
+    fp32 sums of which the second may cancel, 128 e, and half a step of the type."""
+    rng = np.random.default_rng(hidden)
+    h = np.ldexp(rng.choice([-1.0, 1.0], (5, hidden)), power)
+    dxn, g = rng.integers(-8, 9, (5, hidden)).astype(np.float64), rng.choice([0.5, 1.0, 2.0], hidden)
+    dx, dg = gradients(ctx, h, g, dxn, 0.0, dtype)
+    want, dgw = O.norm_grad(h, g, 0.0, dxn, 0.0)
+    u = np.abs(dxn * g)
+    size = np.ldexp(u + np.mean(u, axis=1, keepdims=True), -power)
+    assert (np.abs(dx - want) <= 128 * E * size + (2.0 ** -8 if dtype == "bf16" else E) * np.abs(want)).all()
+    assert np.array_equal(dg, dgw)          # sums of a few whole numbers
