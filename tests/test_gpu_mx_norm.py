@@ -47,3 +47,19 @@ def test_rows_whose_inverse_root_has_no_square(ctx, dtype, hidden, power):
     size = np.ldexp(u + np.mean(u, axis=1, keepdims=True), -power)
     assert (np.abs(dx - want) <= 128 * E * size + (2.0 ** -8 if dtype == "bf16" else E) * np.abs(want)).all()
     assert np.array_equal(dg, dgw)          # sums of a few whole numbers
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("rows,hidden", [(300, 1032), (512, 2048), (77, 20001), (17, 12288)])
+def test_partial_sums_of_the_gain_lose_nothing(ctx, dtype, rows, hidden):
+    """Rows of +-1 without eps, so that r is 1, and at most as many rows as partial sums: dg is a sum of the whole numbers in dxn, of 2^24 and of
+    ones, which 24 bits do not hold on the way; rounded once."""
+    rng = np.random.default_rng(rows)
+    h = rng.choice([-1.0, 1.0], (rows, hidden))
+    term = rng.choice([-1.0, 1.0], (rows, hidden))
+    for sign in (1, -1):      # the largest two cancel in some columns
+        at = rng.permuted(np.arange(rows)[:, None].repeat(hidden, axis=1), axis=0)[:2]
+        np.put_along_axis(term, at, np.stack((np.full(hidden, 2.0 ** 24), rng.choice([1.0, -1.0], hidden) * 2.0 ** 24)), axis=0)
+        term *= sign
+        _, dg = gradients(ctx, h, np.ones(hidden), term * h, 0.0, dtype)
+        assert np.array_equal(dg, term.sum(axis=0).astype(np.float32))
