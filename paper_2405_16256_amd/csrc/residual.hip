@@ -49,19 +49,34 @@ template <bool RAGGED> __device__ __forceinline__ int chunk_values(int hidden, i
 template <typename T> __device__ __forceinline__ T* chunk_at(T* row, int at) { return (T*)((char*)row + (uint32_t)at * (uint32_t)sizeof(T)); }
 template <typename T> __device__ __forceinline__ const T* chunk_at(const T* row, int at) { return (const T*)((const char*)row + (uint32_t)at * (uint32_t)sizeof(T)); }
 
-// r = 1 / sqrt(ss / hidden + eps).  The division of a root rounds twice; a step of Newton's, with a r's rounding carried along, leaves little more
-// than half a step: 4096x12288 bf16, values of xn that round otherwise than in 64 bits 7.9e-6 -> 7.4e-6 of them at the same time.  At
-// 0 and at infinity, where the step is NaN, r stays.
-__device__ __forceinline__ float inverse_root(float ss, int hidden, float eps) {
-    const float a = ss / (float)hidden + eps, r = 1.0f / sqrtf(a), x = a * r;
-    const float better = fmaf(0.5f * r, fmaf(-x, r, 1.0f) - fmaf(a, r, -x) * r, r);
-    return better > 0.f ? better : r;
+// r = 1 / sqrt(ss / hidden + eps).  What a row's values have in common, the lanes' sums and r, is carried in 64 bits, r as the sum of two floats: a value
+// of xn is rounded twice then, v r and the product with g.  4096x12288 bf16, of 1e6 values of xn 5.4 round otherwise than in 64 bits (7.5 with fp32 sums and
+// root), at the same time; rows of 512 lose most, 8192x512 8.9 -> 9.2 us.
+template <int W>
+__device__ __forceinline__ double lanes_sum(float lane, double (&red)[W]) {
+    double s = lane;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
+    if (W == 1) return s;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < W; i++) s += red[i];
+    return s;
+}
+struct Root { float hi, lo; };
+__device__ __forceinline__ Root split_inverse_root(double ss, int hidden, float eps) {
+    const double a = ss / hidden + eps, x = __builtin_amdgcn_rsq(a), better = fma(0.5 * x, fma(-a * x, x, 1.0), x);
+    const double r = better > 0.0 ? better : x;   // at 0 and at infinity, where Newton's step is NaN
+    const float hi = (float)r;
+    return Root{hi, hi < INFINITY ? (float)(r - hi) : 0.f};
 }
 
 template <typename T, int W, int CH, bool RAGGED, bool STREAM>
 __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int rows, int hidden, int width, float eps, const T* x, const T* b,
                                                                      const T* __restrict__ g, T* h, T* xn, int format, uint8_t* codes, uint8_t* scales) {
-    __shared__ float red[W];
+    __shared__ double red[W];
     const int t = (int)threadIdx.x & (64 * W - 1);
     const int row = (int)blockIdx.x * rows_each<W>() + (W == 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0);
     if (row >= rows) return;   // one wave a row: no barrier follows
@@ -102,15 +117,14 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
 #pragma unroll
         for (int i = 0; i < 8; i++) ss = fmaf(v[c][i], v[c][i], ss);
     }
-    ss = W == 1 ? wave_sum(ss) : block_sum<W>(ss, red);
-    const float r = inverse_root(ss, hidden, eps);
+    const Root r = split_inverse_root(lanes_sum<W>(ss, red), hidden, eps);
 #pragma unroll
     for (int c = 0; c < CH; c++) {
         const int group = t + 64 * W * c, n = chunk_values<RAGGED>(hidden, 8 * group);
         float u[8];
         rg[c].widen(u);
 #pragma unroll
-        for (int i = 0; i < 8; i++) u[i] = i < n ? v[c][i] * r * u[i] : 0.f;   // past the end also where r is no number
+        for (int i = 0; i < 8; i++) u[i] = i < n ? fmaf(v[c][i], r.hi, v[c][i] * r.lo) * u[i] : 0.f;   // past the end also where r is no number
         if (xn && n > 0) {
             Eight<T> e;
             e.round(u);
@@ -166,6 +180,13 @@ hipError_t add_norm_fwd(int dtype, const Drop& d, int rows, int hidden, float ep
 }
 
 // ------------------------------------------------------------------ gradients
+// The division of a root rounds twice; a step of Newton's, with a r's rounding carried along, leaves little more than half a step.  At 0 and at
+// infinity, where the step is NaN, r stays.
+__device__ __forceinline__ float inverse_root(float ss, int hidden, float eps) {
+    const float a = ss / (float)hidden + eps, r = 1.0f / sqrtf(a), x = a * r;
+    const float better = fmaf(0.5f * r, fmaf(-x, r, 1.0f) - fmaf(a, r, -x) * r, r);
+    return better > 0.f ? better : r;
+}
 // One row's share of dx, db and dg: eight values of h (a), dxn (u), g (w) and dh (o, which becomes dx).
 __device__ __forceinline__ void norm_grad8(const float* a, const float* u, const float* w, float* o, float* sum, float r, float k) {
 #pragma unroll

@@ -63,3 +63,22 @@ def test_partial_sums_of_the_gain_lose_nothing(ctx, dtype, rows, hidden):
         term *= sign
         _, dg = gradients(ctx, h, np.ones(hidden), term * h, 0.0, dtype)
         assert np.array_equal(dg, term.sum(axis=0).astype(np.float32))
+
+
+@pytest.mark.parametrize("rows,hidden", [(4096, 12288), (12500, 4000), (48001, 1000)])
+def test_normed_values_are_rounded_twice(ctx, rows, hidden):
+    """What rounds to bf16 otherwise than in 64 bits.  With v r and its product with g each rounded to fp32, evenly spread within half a step of 2^-24 and
+    a bf16's borders 2^-7 apart, that is the mean of a sum of two such errors, 2/3 of the half step: 2/3 2^-17 = 5.1e-6 of the values.  A quarter more is
+    left for what the lanes' sums in fp32 add; three such errors would be 6.2e-6 and more, four 7.2e-6."""
+    wrong = 0
+    for seed in range(2):
+        gen = torch.Generator(device=L.DEV).manual_seed(seed)
+        x = torch.randn(rows, hidden, device=L.DEV, generator=gen).bfloat16()
+        g = torch.randn(hidden, device=L.DEV, generator=gen).bfloat16()
+        xn = torch.empty_like(x)
+        hh.hh_add_norm_fwd(ctx, hh.make_add_norm_cfg(rows, hidden, 1e-5), None, x, None, g, None, xn, None, L.stream_ptr())
+        h = x.double()
+        want = h / torch.sqrt(torch.mean(h * h, dim=1, keepdim=True) + float(np.float32(1e-5))) * g.double()
+        wrong += int((xn != want.bfloat16()).sum())
+    print("rounds otherwise: %.2e" % (wrong / (2 * rows * hidden)))
+    assert wrong <= 1.25 * 2 / 3 * 2.0 ** -17 * 2 * rows * hidden
