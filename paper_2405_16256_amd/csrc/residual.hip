@@ -49,12 +49,11 @@ template <bool RAGGED> __device__ __forceinline__ int chunk_values(int hidden, i
 template <typename T> __device__ __forceinline__ T* chunk_at(T* row, int at) { return (T*)((char*)row + (uint32_t)at * (uint32_t)sizeof(T)); }
 template <typename T> __device__ __forceinline__ const T* chunk_at(const T* row, int at) { return (const T*)((const char*)row + (uint32_t)at * (uint32_t)sizeof(T)); }
 
-// r = 1 / sqrt(ss / hidden + eps).  What a row's values have in common, the lanes' sums and r, is carried in 64 bits, r as the sum of two floats: a value
-// of xn is rounded twice then, v r and the product with g.  4096x12288 bf16, of 1e6 values of xn 5.4 round otherwise than in 64 bits (7.5 with fp32 sums and
-// root), at the same time; rows of 512 lose most, 8192x512 8.9 -> 9.2 us.
+// r = 1 / sqrt(ss / hidden + eps).  What a row's values have in common, the sums of eight squares each and r, is carried in 64 bits, r as the sum of two
+// floats: a value of xn is rounded twice then, v r and the product with g.  4096x12288 bf16, of 1e6 values of xn 4.7 round otherwise than in 64 bits (7.5
+// with fp32 sums and root), at the same time; rows of 512 lose most, 8192x512 8.9 -> 9.2 us.
 template <int W>
-__device__ __forceinline__ double lanes_sum(float lane, double (&red)[W]) {
-    double s = lane;
+__device__ __forceinline__ double lanes_sum(double s, double (&red)[W]) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, WAVE);
     if (W == 1) return s;
@@ -66,15 +65,28 @@ __device__ __forceinline__ double lanes_sum(float lane, double (&red)[W]) {
     return s;
 }
 struct Root { float hi, lo; };
-__device__ __forceinline__ Root split_inverse_root(double ss, int hidden, float eps) {
-    const double a = ss / hidden + eps, x = __builtin_amdgcn_rsq(a), better = fma(0.5 * x, fma(-a * x, x, 1.0), x);
+__device__ __forceinline__ Root split_inverse_root(double ss, double per_value, float eps) {
+    const double a = fma(ss, per_value, (double)eps), x = __builtin_amdgcn_rsq(a), better = fma(0.5 * x, fma(-a * x, x, 1.0), x);
     const double r = better > 0.0 ? better : x;   // at 0 and at infinity, where Newton's step is NaN
     const float hi = (float)r;
     return Root{hi, hi < INFINITY ? (float)(r - hi) : 0.f};
 }
 
+// v r g for packing, near a border between two numbers of a format: on the side where the unrounded product lies, that is, with what is left of it behind
+// the last bit as that bit.  Rounded to fp32 first, 4.8e-7 of the values that become E4M3 lie on a border, and half of them on its wrong side, which is
+// a step of the format; so 44 of 1e8 were wrong, and 2 are.  4096x12288 with E4M3 79.5 -> 80.4 us, 256x4096 with E2M1 5.2 -> 5.5.
+__device__ __forceinline__ float normed_odd(float v, const Root& r, float g) {
+    const float y = v * r.hi, y_rest = fmaf(v, r.lo, fmaf(v, r.hi, -y)), u = y * g, u_rest = fmaf(y_rest, g, fmaf(y, g, -u));
+    const float s = u + u_rest, rest = (u - s) + u_rest;
+    constexpr int NORMAL_OR_DENORMAL = 0x198;   // of either sign
+    if (!__builtin_amdgcn_classf(u_rest, NORMAL_OR_DENORMAL)) return u;   // an infinity, what is no number, and zeros with their sign
+    if (fabsf(rest) <= fabsf(s) * 0x1p-40f) return s;   // s itself, but for the roundings in 64 bits
+    const uint32_t w = __float_as_uint(s);
+    return __uint_as_float((w - ((w ^ __float_as_uint(rest)) >> 31)) | 1u);
+}
+
 template <typename T, int W, int CH, bool RAGGED, bool STREAM>
-__global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int rows, int hidden, int width, float eps, const T* x, const T* b,
+__global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int rows, int hidden, int width, float eps, double per_value, const T* x, const T* b,
                                                                      const T* __restrict__ g, T* h, T* xn, int format, uint8_t* codes, uint8_t* scales) {
     __shared__ double red[W];
     const int t = (int)threadIdx.x & (64 * W - 1);
@@ -99,10 +111,12 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
         }
     }
     const uint64_t offset = b && d.dropped ? drop_offset(d) : 0;
-    float v[CH][8], ss = 0.f;
+    float v[CH][8];
+    double ss = 0.0;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
         const int group = t + 64 * W * c, n = chunk_values<RAGGED>(hidden, 8 * group);
+        float squares = 0.f;
         rx[c].widen(v[c]);
         if (b && n > 0) {
             float u[8];
@@ -115,9 +129,10 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
             rx[c].widen(v[c]);   // the norm is of the sum as it is kept
         }
 #pragma unroll
-        for (int i = 0; i < 8; i++) ss = fmaf(v[c][i], v[c][i], ss);
+        for (int i = 0; i < 8; i++) squares = fmaf(v[c][i], v[c][i], squares);
+        ss += squares;
     }
-    const Root r = split_inverse_root(lanes_sum<W>(ss, red), hidden, eps);
+    const Root r = split_inverse_root(lanes_sum<W>(ss, red), per_value, eps);
 #pragma unroll
     for (int c = 0; c < CH; c++) {
         const int group = t + 64 * W * c, n = chunk_values<RAGGED>(hidden, 8 * group);
@@ -131,6 +146,15 @@ __global__ __launch_bounds__(row_threads<W>()) void k_add_norm_fwd(Drop d, int r
             e.template store<STREAM>(chunk_at(xn_row, 8 * group), n);
         }
         if (format != MX_NONE && 8 * group < width) {   // whole blocks of 32: the four lanes of one are here together
+            // Borders (of normal numbers) end in 19 zeros at least, and two roundings are off by two last bits at most.
+            uint32_t least = ~0u;
+#pragma unroll
+            for (int i = 0; i < 8; i++) least = min(least, (__float_as_uint(u[i]) + 2u) << 13);
+            if (__builtin_expect(least <= 4u << 13, 0)) {
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if ((__float_as_uint(u[i]) + 2u) << 13 <= 4u << 13 && i < n) u[i] = normed_odd(v[c][i], r, rg[c].at(i));
+            }
             const uint32_t m = quad_max(magnitude8(u));
             const Pair<float> pairs[4] = {{u[0], u[1]}, {u[2], u[3]}, {u[4], u[5]}, {u[6], u[7]}};
             uint32_t byte;
@@ -154,7 +178,7 @@ static hipError_t fwd(const Drop& d, int rows, int hidden, float eps, const void
     const int width = format == MX_NONE ? 0 : (int)mx_width(hidden), chunks = format == MX_NONE ? (hidden + 7) / 8 : width / 8;
     const bool stream = (double)rows * hidden * sizeof(T) * (1 + 2 * (b != nullptr) + (xn != nullptr)) > STREAM_BYTES;
     auto run = [&](auto kern, int each, int threads) {
-        kern<<<(rows + each - 1) / each, threads, 0, st>>>(d, rows, hidden, width, eps, (const T*)x, (const T*)b, (const T*)g, (T*)h, (T*)xn, format,
+        kern<<<(rows + each - 1) / each, threads, 0, st>>>(d, rows, hidden, width, eps, 1.0 / hidden, (const T*)x, (const T*)b, (const T*)g, (T*)h, (T*)xn, format,
                                                            q.codes, q.scales);
         return hipGetLastError();
     };

@@ -82,3 +82,59 @@ def test_normed_values_are_rounded_twice(ctx, rows, hidden):
         wrong += int((xn != want.bfloat16()).sum())
     print("rounds otherwise: %.2e" % (wrong / (2 * rows * hidden)))
     assert wrong <= 1.25 * 2 / 3 * 2.0 ** -17 * 2 * rows * hidden
+
+
+def borders(fmt):
+    n = torch.from_numpy(O.numbers(fmt)).to(L.DEV)
+    return n, (n[1:] + n[:-1]) / 2
+
+
+@pytest.mark.parametrize("fmt", (O.E4M3, O.E2M1))
+@pytest.mark.parametrize("dtype,rows,hidden", [("bf16", 4096, 12288), ("f32", 12500, 4000), ("bf16", 50000, 512)])
+def test_packed_rows_are_those_of_the_unrounded_norm(ctx, dtype, rows, hidden, fmt):
+    """Values of fp32 lie 2^-23 apart and those of a format 2^-3 (E2M1: 2^-1) at most: rounding to fp32 first puts 2^-20 (2^-22) of them on a border
+    between two of its numbers, half of them on its wrong side.  Where packing goes by the unrounded value none are wrong, but for the lanes' sums in
+    fp32, whose errors are below 2^-26 on the mean: an eighth of a rounding's.  A sixth of 2^-21 (2^-23), and three more, are left."""
+    dt, code = TYPES[dtype]
+    f = {O.E4M3: hh.HH_MX_E4M3, O.E2M1: hh.HH_MX_E2M1}[fmt]
+    number, border = borders(fmt)
+    power = torch.tensor([2.0 ** (i - 127) for i in range(255)], dtype=torch.float64, device=L.DEV)   # exact, which the device's own are not
+    wrong = 0
+    for seed in range(2):
+        gen = torch.Generator(device=L.DEV).manual_seed(seed)
+        x = torch.randn(rows, hidden, device=L.DEV, generator=gen).to(dt)
+        g = (1 + 0.1 * torch.randn(hidden, device=L.DEV, generator=gen)).to(dt)
+        c, s = hh.hh_mx_sizes(f, rows, hidden)
+        q = torch.empty(c, dtype=torch.uint8, device=L.DEV), torch.empty(s, dtype=torch.uint8, device=L.DEV)
+        y = torch.empty(rows, hidden, device=L.DEV)
+        hh.hh_add_norm_fwd(ctx, hh.make_add_norm_cfg(rows, hidden, 1e-5, code, f), None, x, None, g, None, None, hh.make_mx(*q), L.stream_ptr())
+        hh.hh_mx_values(ctx, rows, hidden, f, hh.make_mx(*q), hh.HH_F32, y, hidden, L.stream_ptr())
+        h = x.double()
+        want = h / torch.sqrt(torch.mean(h * h, dim=1, keepdim=True) + float(np.float32(1e-5))) * g.double()
+        want = torch.nn.functional.pad(want, (0, -hidden % 32)).reshape(rows, -1, 32)
+        scale = power[torch.frexp(want.abs().amax(dim=2, keepdim=True))[1].long() - 1 - O.TOP[fmt] + 127]
+        v = want / scale
+        nearest = number[torch.bucketize(v.abs(), border)].copysign(v) * scale
+        wrong += int((y.double() != nearest.reshape(rows, -1)[:, :hidden]).sum())
+    share = 2.0 ** (-21 if fmt == O.E4M3 else -23) * 2 * rows * hidden
+    print("wrong: %d, of a rounding to fp32 %.1f" % (wrong, share))
+    assert wrong <= share / 6 + 3
+
+
+@pytest.mark.parametrize("fmt", (O.E4M3, O.E2M1))
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_packed_rows_of_powers_of_two(ctx, dtype, fmt):
+    """Rows of +-2^k without eps are +-1 times their gain: at the border between two scales, where less by any rounding would be another block."""
+    dt, code = TYPES[dtype]
+    f = {O.E4M3: hh.HH_MX_E4M3, O.E2M1: hh.HH_MX_E2M1}[fmt]
+    rng = np.random.default_rng(4)
+    for hidden in [*range(1, 130), 255, 257, 700, 1003, 1536, 2049, 5000, 12288, 20001, 32767]:
+        sign = rng.choice([-1.0, 1.0], (3, hidden))
+        x = torch.from_numpy(np.ldexp(sign, np.array([[0], [-9], [30]]))).to(L.DEV, dt)
+        g = np.ldexp(1.0, rng.integers(-2, 3, hidden))
+        q = [torch.empty(n, dtype=torch.uint8, device=L.DEV) for n in hh.hh_mx_sizes(f, 3, hidden)]
+        y, xn = torch.empty(3, hidden, device=L.DEV), torch.empty_like(x)
+        hh.hh_add_norm_fwd(ctx, hh.make_add_norm_cfg(3, hidden, 0.0, code, f), None, x, None, torch.from_numpy(g).to(L.DEV, dt), None, xn, hh.make_mx(*q), L.stream_ptr())
+        hh.hh_mx_values(ctx, 3, hidden, f, hh.make_mx(*q), hh.HH_F32, y, hidden, L.stream_ptr())
+        assert np.array_equal(xn.double().cpu().numpy(), sign * g), hidden
+        assert np.array_equal(y.double().cpu().numpy(), O.rounded(sign * g, fmt)), hidden
