@@ -77,8 +77,8 @@ int hh_mx_values(hh_ctx *ctx, int64_t rows, int64_t k, int32_t format, const hh_
 
 /* Residual addition and norm:
  *     h = x + dropout(b)  rounded to dtype,   xn = h g / sqrt(mean(h^2) + eps)
- * x, b, h, xn: [rows, hidden] contiguous; g: [hidden]; all of dtype, arithmetic and statistics in fp32.  b NULL: h is x, which is not
- * written again (h has to be NULL).  h may be x or b.  xn is written where it is not NULL; q receives xn, before it is rounded to dtype,
+ * x, b, h, xn: [rows, hidden] contiguous; g: [hidden]; all of dtype, arithmetic in fp32, a row's sum and root in 64 bits from eight values on.  b NULL: h is x, which is not
+ * written again (h has to be NULL).  h may be x or b.  xn is written where it is not NULL; q receives xn, before it is rounded,
  * packed in `format` (HH_MX_NONE: q has to be NULL).  One of xn and q at least.  drop NULL: nothing is dropped. */
 typedef struct {
     int32_t rows, hidden;  /* hidden: 1 .. 32768; rows: 1 .. 2^24, 2^34 values at most */

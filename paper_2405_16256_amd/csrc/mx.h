@@ -10,9 +10,12 @@ namespace hh {
 // The memory unit takes 16-byte accesses at the alignment of their elements; where a row is aligned they cost no more for being written so.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));   // a bfloat16's alignment
-// STREAM: the launch reads and writes more than the last-level cache keeps for the next one anyway (STREAM_BYTES).  Past the caches, cold
-// tensors: dropout of 4096x12288 bf16 39.1 -> 36.6 us, residual addition with norm and packing 117 -> 105.  Smaller ones are read by what
-// follows while they are there.
+// STREAM: a launch of more than STREAM_BYTES goes past the caches.  Cold tensors: dropout of 4096x12288 bf16 39.1 -> 36.6 us, residual addition
+// with norm and packing 117 -> 105.  The last-level cache holds more than that, so it could cost a call that reads what the one before
+// wrote; a residual connection with its E2M1 projection, forward and backward, takes 1103 us (4096 tokens, 12288 x 8192; 1133 through
+// the caches), 688 (2048 tokens; 697), 531 (4096, 4096 x 11008; 539), 434 (8192, 4096 x 4096; 448).  Its forward half alone loses once in these
+// four, 4096 tokens of 4096 x 11008, 149 us in place of 143.  Rows that end inside a chunk and the longest rows' gradients, which are read twice,
+// go through the caches.
 constexpr double STREAM_BYTES = 96e6;
 template <bool STREAM, typename V>
 __device__ __forceinline__ V load_any(const V* p) { return STREAM ? __builtin_nontemporal_load(p) : *p; }

@@ -12,8 +12,9 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // ------------------------------------------------------------------ few rows
 // C of up to 16 TM rows: 16 columns a workgroup, its waves take 256 k at a time in turn, straight from memory into registers, and their sums
 // meet in LDS.  Bound by the one read of B: nothing of it is used twice, so it has no use for LDS, and what counts is that every wave of the
-// chip has its whole share under way at once: 1x4096x11008 E4M3 by E2M1 6.5 us (23 MB, 3.6 TB/s; a launch that does nothing is 2 of them),
-// E2M1 twice 5.9; 16 rows of 4096x4096 4.7 to 6.6.
+// chip has its whole share under way at once: 1x4096x11008 E4M3 by E2M1 7.6 us (24 MB, 3.2 TB/s; a launch that does nothing is 2 of them).  One
+// after another, with B from memory, 8.6, E2M1 twice 7.8, E4M3 twice 14.5 (3.2 TB/s); of 32 rows 18.8, 13.0, 25.0: what else there is, and
+// widening on either side.
 //
 // Of 16 rows x 128 k lane l holds row l % 16 and, with q = l / 16, the codes 32 q .. 32 q + 31 with their one scale: of E2M1 on both sides what the
 // matrix instruction takes, otherwise (WIDE) eight at a time, widened, whatever k they are of, the same for both operands.
@@ -134,8 +135,9 @@ __global__ __launch_bounds__(64 * NW) void k_product_rows(MxRowsProblem p) {
 // global memory; a row of a stage is KS bytes of E4M3 or KS / 2 of E2M1 (KS 128, or 256), and the scales of those k lie behind the
 // tiles.  16-byte chunks are XOR-swizzled by the row so that a fragment's 16 lanes cover all banks.
 //
-// 4096x8192x12288 into bf16: E2M1 214 us (3.85 PFLOP/s), E4M3 355 (2.32), E4M3 by E2M1 317 (2.6), widened into fp32 606 (1.36).  The matrix
-// cores alone, with random operands in registers, reach 6.8, 4.0 and (bf16) 1.8 PFLOP/s under the power limit.  Counters (E2M1): matrix
+// 4096x8192x12288 into bf16: E2M1 223 us (3.70 PFLOP/s; 214 to 223 from card to card), with fast sums E4M3 376 (2.19) and E4M3 by E2M1 318
+// (2.60), widened 601 (1.37) and 574 (1.44), widened into fp32 595 (1.39).  The matrix cores alone, with random operands in registers, reach
+// 6.8, 4.0 (both with an E4M3 operand) and (bf16) 1.8 PFLOP/s under the power limit.  Counters (E2M1, where it took 214): matrix
 // cores busy 51 % of the cycles at 1.85 GHz, workgroups there 91 % (two tiles a compute unit, each with its start and end), waits 33 %,
 // for LDS 3 %.  Without the loop's requests it takes 168 us, without the matrix instructions 165, with every request in L2 203: neither
 // side is the limit by itself, and the two add up to more than either.  Four waves of 128x128, four stages of 128 k (268), fragments fetched
@@ -470,8 +472,8 @@ __global__ __launch_bounds__(256) void k_sum_shares(const float* __restrict__ pa
 // Which kernel takes a product, and how many shares of k: the least predicted time.  A workgroup of tiles takes ENDS_US to start and to write
 // its tile and STAGE_US a stage (256 k of E2M1, else 128), the same alone on its compute unit as beside another one; shares cost a second
 // launch and the traffic of their sums.  Against the best of all plans, at 64 shapes and formats of 40 to 8192 rows, it is within 5 % in 59
-// of them and 15 % off at worst; 1003x700x2050, E4M3 by E2M1: tiles of 64 6.5 us, of 128 11.0, of 256 24; 2048x4096x4096 65, 43.5, 45;
-// 4096x4096x4096 118, 87, 59.5.
+// of them and 15 % off at worst; 1003x700x2050, E4M3 by E2M1 with fast sums and operands in the caches: tiles of 64 6.5 us, of 128 11.0, of 256
+// 24; 2048x4096x4096 65, 43.5, 45; 4096x4096x4096 118, 87, 59.5.
 enum { ROWS_16, ROWS_32, TILES_64, TILES_128, TILES_256 };
 struct MxPlan { int kernel, split; };
 // The instruction for E4M3 adds its products in fewer bits than fp32's: taken only where the caller allows it, the result has fewer still and it is
@@ -556,11 +558,11 @@ size_t mx_product_workspace(const MxProduct& p) {
 
 template <int FA, int FB, bool WIDE, typename TC>
 static hipError_t run_product(const MxProduct& p, void* ws, hipStream_t st) {
-    // Stages: three hide a request's way where LDS has room for them, which it has where one side is half the bytes (4096x8192x12288 E4M3 by
-    // E2M1 322 -> 306 us), for tiles of 64 (four are 2 % slower, two up to 30 %), and for one workgroup of tiles of 128 on a compute unit
-    // (2048x2048x8192 E4M3 57.4 -> 45.0), where a second one does so too (2048x4096x4096, two of them: 47.7, one at a time 50.3).  Tiles of 64
-    // that are widened do better with two stages of 256 k, half as many ends of one (1024x1024x4096 18.5 -> 16.3 us, 1003x700x2050 11.2 -> 10.4);
-    // the others do not (11.2 and 12.1, 7.3 and 7.9).
+    // Stages (operands in the caches, fast sums but where they are widened): three hide a request's way where LDS has room for them, which it has
+    // where one side is half the bytes (4096x8192x12288 E4M3 by E2M1 5 % faster), for tiles of 64 (four are 2 % slower, two up to 30 %), and for one
+    // workgroup of tiles of 128 on a compute unit (2048x2048x8192 E4M3 57.4 -> 45.0), where a second one does so too (2048x4096x4096, two of
+    // them: 47.7, one at a time 50.3).  Tiles of 64 that are widened do better with two stages of 256 k, half as many ends of one (E4M3 by E2M1
+    // 1024x1024x4096 18.5 -> 16.3 us, 1003x700x2050 11.2 -> 10.4); the others do not (11.2 and 12.1, 7.3 and 7.9).
     constexpr int NS = FA == FB ? 2 : 3, KS = STAGE_K<FA, FB>;
     const MxPlan l = plan(p);
     switch (l.kernel) {

@@ -37,8 +37,8 @@ hipError_t dropout(int dtype, const Drop& d, long rows, long cols, const void* x
 
 // ------------------------------------------------------------------ residual and norm
 // h = x + dropout(b), r = 1 / sqrt(mean h^2 + eps), xn = h r g: a row stays in registers from its sum to its packed copy, so that each tensor
-// is read or written once.  Bound by memory: 4096x12288 bf16 with dropout, h, xn and E4M3 written 77.6 us (5.9 TB/s); one row of 4096 2.9 us,
-// a launch and a chain of loads, two barriers and stores.
+// is read or written once.  Bound by memory: 4096x12288 bf16 with dropout, h, xn and E4M3 written 77.8 us (5.8 TB/s); rows of 32768, 2048 of them,
+// bf16 105 us, fp32 227 (5.1 and 4.7 TB/s); one row of 4096 3.2 us, a launch and a chain of loads, two barriers and stores.
 // W waves a row, CH chunks of eight values a lane: chunk t + 64 W c.  Four rows to a workgroup where a wave takes one.
 template <int W> constexpr int row_threads() { return W == 1 ? 256 : 64 * W; }
 template <int W> constexpr int rows_each() { return W == 1 ? 4 : 1; }
@@ -73,7 +73,7 @@ __device__ __forceinline__ Root split_inverse_root(double ss, double per_value, 
 }
 
 // v r g for packing, near a border between two numbers of a format: on the side where the unrounded product lies, that is, with what is left of it behind
-// the last bit as that bit.  Rounded to fp32 first, 4.8e-7 of the values that become E4M3 lie on a border, and half of them on its wrong side, which is
+// the last bit as that bit.  Rounded to fp32 first, 9.5e-7 of the values that become E4M3 lie on a border, and half of them on its wrong side, which is
 // a step of the format; so 44 of 1e8 were wrong, and 2 are.  4096x12288 with E4M3 79.5 -> 80.4 us, 256x4096 with E2M1 5.2 -> 5.5.
 __device__ __forceinline__ float normed_odd(float v, const Root& r, float g) {
     const float y = v * r.hi, y_rest = fmaf(v, r.lo, fmaf(v, r.hi, -y)), u = y * g, u_rest = fmaf(y_rest, g, fmaf(y, g, -u));
@@ -234,7 +234,7 @@ __device__ __forceinline__ void row_sums(float& ss, float& dot, float (&red)[2][
 }
 
 // With u = dxn g: dx = dh + r (u - h r^2 mean(u h)), db = dropout(dx), dg = sum over rows of dxn h r.  Statistics are formed again from h, which
-// the pass reads anyway.  Bound by memory: 4096x12288 bf16, three tensors read and two written, 95.6 us (5.3 TB/s) and 5.0 for the sums of dg.
+// the pass reads anyway.  Bound by memory: 4096x12288 bf16, three tensors read and two written, 96.1 us (5.2 TB/s) and 5.1 for the sums of dg.
 // Workgroups walk rows p, p + parts, ... (four of them at once where a wave takes one) and keep their sums for dg in registers; partial[p].
 // Registers of bf16 rows are held to what leaves four waves on a SIMD: a row's loads wait for no one but themselves, and the other waves'
 // cover them.
@@ -342,7 +342,8 @@ __global__ __launch_bounds__(row_threads<W>(), (RAGGED ? 2 : grad_waves<T, CH>()
     }
 }
 
-// Rows too long for a workgroup's registers: asked for a second time, which the caches answer, and dg's sums in LDS (up to 128 KB).
+// Rows too long for a workgroup's registers: asked for a second time, which the caches answer, and dg's sums in LDS (up to 128 KB), so that a compute
+// unit has one workgroup, whose loads nothing covers: 4096x16384 fp32 333 us, 2048x32768 bf16 188, fp32 359 (4.0, 3.6 and 3.7 TB/s).
 template <typename T>
 __global__ __launch_bounds__(1024) void k_add_norm_bwd_wide(Drop d, int rows, int hidden, int parts, float eps, const T* h, const T* __restrict__ g,
                                                              const T* dxn, const T* dh, T* dx, T* db, float* __restrict__ partial) {
